@@ -341,6 +341,83 @@ int tilemix_decode_int8kv(const tilemix_decode_t* p, const void* q_f16, const vo
                           float* q_scale_out, void* workspace, size_t workspace_bytes,
                           void* stream);
 
+/* ---- a paged key/value cache: written token by token, read back, attended to ------------------------------------
+ * (The paper has no counterpart: its decode interface, tilemix_decode_int8kv, takes one dense cache per sequence.)
+ * A layer's cache is two pools of pages of page_size tokens and a table that gives each sequence its pages: token j of
+ * sequence b lies in row j % page_size of page block_table[b][j / page_size].  The pools hold
+ *   TILEMIX_CACHE_16BIT  the values, in the type of the activations, or
+ *   TILEMIX_CACHE_INT8   codes x8 with one FP32 scale delta for every (token, head): x8 = round(x / delta) in {-127..127},
+ *                        delta = max|x| / 127 over the token's head_dim values (the quantiser above with blocks of one
+ *                        row); the value is x8 * delta.  A scale per token lets a token be written once: a scale per block
+ *                        would have to requantise the open block with every token that joins it.
+ * Both cache_len and block_table live on the device and are read by the kernels: a CUDA graph that holds these calls can be
+ * replayed while the sequences grow.  A sequence's length is clamped to [0, max_pages * page_size].  A table entry outside
+ * [0, n_pages) is a hole (a page that is not resident): it is never accessed, and its keys are as if they did not exist.
+ * Several sequences may share pages that are only read (a common prefix); a page that is appended to belongs to one. */
+#define TILEMIX_TYPE_FP16 0
+#define TILEMIX_TYPE_BF16 1
+#define TILEMIX_CACHE_16BIT 0
+#define TILEMIX_CACHE_INT8 1
+typedef struct tilemix_paged {
+    int32_t batch, heads_kv, head_dim;
+    int32_t page_size;     /* tokens of a page: 16, 32, 64, 128 or 256                                            */
+    int32_t n_pages;       /* pages of the pools                                                                  */
+    int32_t max_pages;     /* table entries of a sequence                                                         */
+    int32_t act_type;      /* type of queries, new keys and values, outputs: TILEMIX_TYPE_*                       */
+    int32_t cache_type;    /* TILEMIX_CACHE_*                                                                     */
+    int64_t k_stride[3], v_stride[3]; /* of the pools, in elements, for (page, head, token); head_dim is contiguous; all
+                              zeros = dense [n_pages, Hk, page_size, d].  Any order of the three axes, so that no two rows
+                              overlap; strides and bases are multiples of 16 bytes                                 */
+    int64_t table_stride;  /* entries between the rows of block_table; 0 = max_pages                              */
+    void *k_pool, *v_pool;
+    float *k_scale, *v_scale;          /* FP32 [n_pages, Hk, page_size], dense; 16-bit caches: not read, may be NULL  */
+    const int32_t* block_table;        /* int32 [batch, max_pages] on the device                                      */
+    const int32_t* cache_len;          /* int32 [batch] on the device                                                 */
+} tilemix_paged_t;
+
+/* Writes new tokens' keys and values into the cache, quantised if it is INT8.  The new tokens are the LAST ones of their
+ * sequences: cache_len counts them already, so that the same arrays serve the attention that follows.  Row i of the n_b new
+ * rows of sequence b becomes token cache_len[b] - n_b + i.
+ *   k_new, v_new  [n_tokens, Hk, d] in act_type, packed sequence by sequence; strides in elements for (token, head), NULL =
+ *                 dense; 16-byte multiples.  They must not overlap the pools.
+ *   cu_new        int32 [batch + 1] on the DEVICE: sequence b owns the rows [cu_new[b], cu_new[b+1]); non-decreasing from 0;
+ *                 rows from cu_new[batch] on are padding and are not read.  NULL: one new token per sequence (n_tokens == batch)
+ * A row that has no place (a position below 0 or past the table, a hole) is dropped; everything else in the pools stays as it
+ * was.  A row with an infinity or a NaN gets delta = NaN and codes 0: it reads back as NaN.  One kernel. */
+int tilemix_paged_append(const tilemix_paged_t* c, int32_t n_tokens, const void* k_new, const int64_t* k_new_stride,
+                         const void* v_new, const int64_t* v_new_stride, const int32_t* cu_new, void* stream);
+
+/* Reads tokens [start[b], cache_len[b]) of every sequence back, as act_type: the FP32 product x8 * delta, rounded
+ * (16-bit caches: a copy).  The dense form is what tilemix_attention_fwd_chunk takes as K and V, the packed one what the variable-length calls
+ * take.
+ *   start     int32 [batch] on the device, or NULL = 0 (values below 0 count as 0)
+ *   cu_out    NULL: dense outputs [batch, Hk, out_rows, d], token start[b] + i of sequence b in row i; tokens past
+ *             out_rows are left out.  Otherwise int32 [batch + 1] on the DEVICE (as cu_new): packed outputs
+ *             [out_rows, Hk, d], token start[b] + i in row cu_out[b] + i, for rows below cu_out[b+1]
+ *   k_out, v_out  strides in elements for (batch, head, token) -- the batch stride of packed outputs is not used --, NULL =
+ *             dense; 16-byte multiples.  They must not overlap the pools.
+ * Rows of the outputs that no token belongs to are left as they were; a token in a hole reads as zeros.  One kernel. */
+int tilemix_paged_gather(const tilemix_paged_t* c, const int32_t* start, const int32_t* cu_out, int32_t out_rows,
+                         void* k_out, const int64_t* k_out_stride, void* v_out, const int64_t* v_out_stride, void* stream);
+
+/* One new query token per sequence attends to the first cache_len[b] tokens of the cache:
+ *   s_j = scale * (q . k_j),  o = sum_j softmax(s)_j v_j,  lse = ln sum_j exp(s_j),
+ * with the values that the cache stands for; queries are not quantised.  FP32 scores, statistics and sums; the
+ * probabilities are rounded to 16 bits for the product with V.
+ *   heads_q   any multiple of heads_kv
+ *   softmax_scale  <= 0 means 1/sqrt(head_dim)
+ *   q, out    [batch, Hq, d] in act_type; strides in elements for (batch, head), NULL = dense; 16-byte multiples
+ *   lse       nullable FP32 [batch, Hq]
+ *   workspace >= tilemix_paged_decode_workspace_size(c, heads_q) bytes, 16-byte aligned; nothing is kept in it between calls,
+ *             but calls that may run at the same time need one each
+ * A sequence without a key (length 0, or all of it holes) gets a zero row and lse = -inf.  The work is shared out over the
+ * GPU by the lengths that the kernel finds, so the order of the FP32 sums of a row depends on the lengths beside it; it is
+ * the same in every run.  Waits inside the kernel are bounded: where one runs out, the outputs of the rows concerned are NaN. */
+size_t tilemix_paged_decode_workspace_size(const tilemix_paged_t* c, int32_t heads_q);
+int tilemix_paged_decode(const tilemix_paged_t* c, int32_t heads_q, float softmax_scale, const void* q,
+                         const int64_t* q_stride, void* out, const int64_t* out_stride, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
 /* W = ceil(ceil(L / (G*tile_n)) / 32); <= 0 on invalid arguments. */
 int tilemix_mask_words_per_row(int seqlen, int tile_n, int group);
 /* Bytes of `workspace` needed by tilemix_attention_fwd (0 on an invalid problem). */

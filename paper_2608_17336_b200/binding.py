@@ -26,6 +26,7 @@ EXPORTS = (
     "tilemix_pack_routing_mask_varlen", "tilemix_attention_fwd_varlen",
     "tilemix_decode_workspace_size", "tilemix_decode_int8kv", "tilemix_attention_fwd_chunk",
     "tilemix_chunk_v8_workspace_size", "tilemix_attention_fwd_chunk_v8",
+    "tilemix_paged_append", "tilemix_paged_gather", "tilemix_paged_decode", "tilemix_paged_decode_workspace_size",
     "tilemix_test_drop_copy", "tilemix_tensor_peak_probe",
 )
 
@@ -78,6 +79,13 @@ class DecodeStruct(ctypes.Structure):
                                                "group", "mask_batch", "n_splits")] + [("softmax_scale", ctypes.c_float)]
 
 
+class PagedStruct(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "heads_kv", "head_dim", "page_size", "n_pages", "max_pages",
+                                               "act_type", "cache_type")]
+                + [("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("table_stride", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("k_pool", "v_pool", "k_scale", "v_scale", "block_table", "cache_len")])
+
+
 _lib = None
 
 
@@ -126,6 +134,12 @@ def lib() -> ctypes.CDLL:
         L.tilemix_pack_routing_mask_varlen.argtypes = [pp, vlp, vp, u32, vp, vp, vp, ctypes.c_size_t, vp]
         L.tilemix_attention_fwd_varlen.argtypes = [pp, vlp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                                    ctypes.c_size_t, ctypes.POINTER(DebugStruct), vp]
+        gp = ctypes.POINTER(PagedStruct)
+        L.tilemix_paged_append.argtypes = [gp, i32, vp, vp, vp, vp, vp, vp]
+        L.tilemix_paged_gather.argtypes = [gp, vp, vp, i32, vp, vp, vp, vp, vp]
+        L.tilemix_paged_decode_workspace_size.argtypes = [gp, i32]
+        L.tilemix_paged_decode_workspace_size.restype = ctypes.c_size_t
+        L.tilemix_paged_decode.argtypes = [gp, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -461,4 +475,128 @@ def tilemix_attention_fwd_chunk_v8(p: ProblemStruct, kv_len: int, q, k, v8, v_sc
                                               _ptr(q8), _ptr(k8), _ptr(q_scale), _ptr(k_scale), _ptr(words), _ptr(out),
                                               _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
     _check(rc, "tilemix_attention_fwd_chunk_v8")
+    return {"out": out, "lse": lse, "workspace": workspace}
+
+
+# ------------------------------------------------------------------ paged key/value cache
+
+TYPE_FP16, TYPE_BF16 = 0, 1
+CACHE_16BIT, CACHE_INT8 = 0, 1
+_ACT = {torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}
+
+
+class PagedCache:
+    """A layer's paged cache, as paged_cache() describes it; keeps the tensors alive that the C struct points to."""
+    __slots__ = ("struct", "ref", "tensors", "dtype", "device")
+
+
+def paged_cache(k_pool, v_pool, block_table, cache_len, k_scale=None, v_scale=None, dtype=None) -> PagedCache:
+    """Describes a cache: pools [n_pages,Hk,page_size,d] (views with other strides too) of ``dtype`` (FP16 or BF16) or INT8
+    with scales FP32 [n_pages,Hk,page_size]; block_table int32 [B,max_pages] and cache_len int32 [B], both read at every call.
+    ``dtype`` is the type of queries and new tokens (default: that of the pools, FP16 for INT8 pools)."""
+    int8 = k_pool.dtype == torch.int8
+    if dtype is None:
+        dtype = torch.float16 if int8 else k_pool.dtype
+    assert dtype in _ACT and k_pool.dtype in (dtype, torch.int8) and v_pool.dtype == k_pool.dtype
+    assert k_pool.dim() == 4 and v_pool.shape == k_pool.shape and k_pool.stride(3) == 1 and v_pool.stride(3) == 1
+    n_pages, hk, page_size, d = k_pool.shape
+    assert block_table.dtype == torch.int32 and block_table.dim() == 2 and (block_table.stride(1) == 1 or block_table.shape[1] <= 1)
+    B, max_pages = block_table.shape
+    assert cache_len.dtype == torch.int32 and cache_len.shape == (B,) and cache_len.is_contiguous()
+    held = [k_pool, v_pool, block_table, cache_len]
+    if int8:
+        for t in (k_scale, v_scale):
+            assert t is not None and t.dtype == torch.float32 and t.shape == (n_pages, hk, page_size) and t.is_contiguous()
+        held += [k_scale, v_scale]
+    else:
+        assert k_scale is None and v_scale is None, "a 16-bit cache has no scales"
+    dev = k_pool.device
+    assert all(t.is_cuda and t.device == dev for t in held), "all of a cache lies on one CUDA device"
+    c = PagedCache()
+    c.struct = PagedStruct(B, hk, d, page_size, n_pages, max_pages, _ACT[dtype], CACHE_INT8 if int8 else CACHE_16BIT)
+    c.struct.k_stride[:] = k_pool.stride()[:3]
+    c.struct.v_stride[:] = v_pool.stride()[:3]
+    c.struct.table_stride = max(block_table.stride(0), max_pages) if B == 1 else block_table.stride(0)
+    c.struct.k_pool, c.struct.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
+    c.struct.k_scale, c.struct.v_scale = _ptr(k_scale), _ptr(v_scale)
+    c.struct.block_table, c.struct.cache_len = block_table.data_ptr(), cache_len.data_ptr()
+    c.ref, c.tensors, c.dtype, c.device = ctypes.byref(c.struct), tuple(held), dtype, dev
+    return c
+
+
+def _paged_side(c, t, dims, what):
+    """Checks a 16-bit tensor next to the cache; returns its strides for the C call (None where it is dense)."""
+    assert t.dtype == c.dtype and t.device == c.device and t.shape[-1] == c.struct.head_dim and t.dim() == dims, what
+    if t.is_contiguous():
+        return None
+    st = t.stride()
+    assert st[-1] == 1, "head_dim axis must be contiguous"
+    return (ctypes.c_int64 * 3)(*st[:-1])
+
+
+def _paged_index(c, t, n):
+    if t is not None:
+        assert t.dtype == torch.int32 and t.device == c.device and t.shape == (n,) and t.is_contiguous()
+    return _ptr(t)
+
+
+def _paged_call(c, name, *args):
+    """The C call on the current stream of the cache's device."""
+    if c.device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(c.device):
+            rc = getattr(lib(), name)(c.ref, *args, _stream())
+    else:
+        rc = getattr(lib(), name)(c.ref, *args, _stream())
+    _check(rc, name)
+
+
+def tilemix_paged_append(c: PagedCache, k_new, v_new, cu_new=None):
+    """Writes the new tokens k_new, v_new [n,Hk,d] into the cache, as the last ones of their sequences (cache_len counts them
+    already); cu_new int32 [B+1] (CUDA) says whose rows they are, None: one a sequence."""
+    assert k_new.shape == v_new.shape and k_new.shape[1] == c.struct.heads_kv
+    ks, vs = _paged_side(c, k_new, 3, "k_new"), _paged_side(c, v_new, 3, "v_new")
+    _paged_call(c, "tilemix_paged_append", k_new.shape[0], k_new.data_ptr(), ks, v_new.data_ptr(), vs,
+                _paged_index(c, cu_new, c.struct.batch + 1))
+
+
+def tilemix_paged_gather(c: PagedCache, k_out, v_out, start=None, cu_out=None):
+    """Reads tokens [start, cache_len) of every sequence back into k_out, v_out: dense [B,Hk,n,d], or with cu_out (int32 [B+1],
+    CUDA) packed [n,Hk,d].  Rows that no token belongs to are left as they were.  Returns (k_out, v_out)."""
+    s = c.struct
+    assert k_out.shape == v_out.shape
+    dims = 4 if cu_out is None else 3
+    ks, vs = _paged_side(c, k_out, dims, "k_out"), _paged_side(c, v_out, dims, "v_out")
+    if cu_out is None:
+        assert k_out.shape[0] == s.batch and k_out.shape[1] == s.heads_kv
+        n = k_out.shape[2]
+    else:
+        assert k_out.shape[1] == s.heads_kv
+        n = k_out.shape[0]
+        ks, vs = (st and (ctypes.c_int64 * 3)(0, st[1], st[0]) for st in (ks, vs))     # (batch, head, token)
+    _paged_call(c, "tilemix_paged_gather", _paged_index(c, start, s.batch), _paged_index(c, cu_out, s.batch + 1), n,
+                k_out.data_ptr(), ks, v_out.data_ptr(), vs)
+    return k_out, v_out
+
+
+def tilemix_paged_decode_workspace_size(c: PagedCache, heads_q: int) -> int:
+    return int(lib().tilemix_paged_decode_workspace_size(c.ref, heads_q))
+
+
+def tilemix_paged_decode(c: PagedCache, q, out=None, want_lse=False, softmax_scale=0.0, workspace=None):
+    """One decode step: q [B,Hq,d] attends to the cache.  Returns a dict: out [B,Hq,d], lse [B,Hq] FP32 (if asked), workspace."""
+    s = c.struct
+    assert q.shape[0] == s.batch
+    qs = _paged_side(c, q, 3, "q")
+    hq = q.shape[1]
+    if out is None:
+        out = torch.empty((s.batch, hq, s.head_dim), dtype=c.dtype, device=c.device)
+    assert out.shape == q.shape
+    os_ = _paged_side(c, out, 3, "out")
+    lse = torch.empty((s.batch, hq), dtype=torch.float32, device=c.device) if want_lse else None
+    if workspace is None:
+        workspace = torch.empty(max(tilemix_paged_decode_workspace_size(c, hq), 16), dtype=torch.uint8, device=c.device)
+    else:
+        assert workspace.device == c.device and workspace.is_contiguous()
+    _paged_call(c, "tilemix_paged_decode", hq, softmax_scale, q.data_ptr(), qs, out.data_ptr(), os_, _ptr(lse),
+                workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return {"out": out, "lse": lse, "workspace": workspace}
