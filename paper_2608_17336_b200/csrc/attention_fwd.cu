@@ -1386,6 +1386,16 @@ int encode_rows_map(CUtensorMap* tm, const void* base, int d, int L, int H, int 
     return rc ? rc : encode_map(enc, tm, base, 2, d, L, H, B, stride_elems, d, box_rows, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+// 4-D map over a pool of pages (innermost first: d, token, head, page); box = 128 bytes of d at most, box_rows tokens, swizzled.
+int encode_pool_map(CUtensorMap* tm, const void* base, int elem_bytes, int d, int page_size, int H, int n_pages,
+                    const int64_t stride_elems[3], int box_rows) {
+    EncodeTiledFn enc = nullptr;
+    const int rc = get_encoder(&enc);
+    const int box_d = d * elem_bytes > 128 ? 128 / elem_bytes : d;
+    return rc ? rc : encode_map(enc, tm, base, elem_bytes, d, page_size, H, n_pages, stride_elems, box_d, box_rows,
+                                box_d * elem_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
 int launch_attention(const Geometry& g, const void* q, const void* k, const void* v, const int8_t* q8,
                      const int8_t* k8, const float* qs, const float* ks, const uint32_t* words, void* out,
                      float* lse, void* workspace, const tilemix_debug_t* dbg, cudaStream_t stream,

@@ -94,6 +94,9 @@ int launch_quantize_pair(const void* q, const int64_t qstride[3], int Hq, int bl
                          int total_blk_q = 0, int total_blk_k = 0);
 // Tensor map over an FP16 [B, H, L, d] operand whose box is box_rows whole rows, unswizzled (attention_fwd.cu).
 int encode_rows_map(CUtensorMap* tm, const void* base, int d, int L, int H, int B, const int64_t stride_elems[3], int box_rows);
+// Tensor map over a pool of pages of a paged cache, element strides (page, head, token) (attention_fwd.cu).
+int encode_pool_map(CUtensorMap* tm, const void* base, int elem_bytes, int d, int page_size, int H, int n_pages,
+                    const int64_t stride_elems[3], int box_rows);
 int launch_pack(const Geometry& g, const uint8_t* route, uint32_t pack_flags, uint32_t* words,
                 unsigned long long* counts, cudaStream_t stream, const VarlenDev* vl = nullptr);
 int launch_attention(const Geometry& g, const void* q, const void* k, const void* v,

@@ -1,8 +1,34 @@
 // Decode step over a paged key/value cache: one query token per sequence.
+//
+// HBM-bound: a cached (token, KV head) is 4 d bytes (16-bit cache) or 2 (d + 4) (INT8 codes and scales), read once, and serves
+// the R = H_q / H_k query heads of its group with 4 R d multiply-adds, far below the tensor cores' rate for R <= 16.  Hence
+// warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
+// at the cost of ~17 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.
+//
+// Layout of the work.  A warp owns a ring of three 8 KB stages and takes CHUNKS of 16 to 64 keys (4 KB of keys, 4 KB of values),
+// which one TMA box a page brings in, swizzled; no warp waits for another but at the end of a row.  Four warps are a CTA,
+// two CTAs share an SM: 192 KB on the way.  Four neighbouring chunks are a UNIT; the units of all (sequence, KV head) rows,
+// one row behind the other, are dealt out to the CTAs in equal runs, so that a batch of unequal lengths keeps every SM busy to
+// the end.  A CTA finds its run from the lengths, which only the device knows.  Rows inside its run it finishes itself; of
+// a row that it shares with its neighbours it leaves a partial result (m, z, O) to the joining kernel.  The ring runs
+// on across rows.
+//
+// Products.  S^T = K Q^T with the KEYS as the 16 rows of the MMA and eight query heads as its columns, then O^T = V^T P^T with
+// the head dimension as the rows: nothing of a 16-row operand is wasted on absent query heads, and O^T takes D / 32 * 8
+// registers for eight heads.  The score fragment (rows keys, columns queries) becomes the right operand of the second product by
+// transposing its 8x8 blocks (movmatrix).
+//
+// INT8 codes become FP16 exactly: byte x + 128 under the exponent byte 0x64 is 1024 + (x + 128), less 1152.  The contraction
+// index may be permuted as long as both operands agree, so a lane takes whole 16-byte pieces of a row; the keys of a block are
+// permuted (key_of_row) so that those loads, of the keys and of the values, touch every bank once.
 #include <math.h>
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "paged.cuh"
+#include "ptx_sm100.cuh"
+#include "softmax_tile.cuh"
 
 namespace tilemix {
 
@@ -10,80 +36,790 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kStages = 3, kStageBytes = 8192, kRingBytes = kWarps * kStages * kStageBytes, kSmemBytes = kRingBytes + 1024;
+constexpr int kCtasPerSm = 2, kSms = 148;
+constexpr int kMaxBoxes = 4;            // pages of a chunk: at most 64 keys in pages of 16
 
 struct PagedDecodeParams {
     PagedCache c;
     int Hq, R;                      // query heads, query heads per KV head
+    int groups, HG;                 // groups of up to 8 NB query heads per KV head; rows of a sequence (Hk * groups)
     float scale_log2;
     const uint8_t* q;
     uint8_t* out;
     int64_t qs[2], os[2];           // bytes: (batch, head)
     float* lse;
+    int4* join;                     // [CTAs]: what the joining kernel has to do, see there
+    float4* part_o;                 // [2 CTAs][D / 16][NB][32 lanes]: accumulator fragments
+    float2* part_mz;                // [2 CTAs][8 NB]: maximum (log2 domain) and sum
+    unsigned long long wait_limit_ns;
+    int drop_chunk;                 // testing aid: every warp leaves out the copies of its chunk of this number (-1: none)
 };
 
-// Plain form: one CTA per query head, a warp takes every fourth key, its lanes the head dimension.
-template <class T, int D, bool INT8>
-__global__ void __launch_bounds__(128)
-paged_decode_kernel(const PagedDecodeParams prm) {
-    constexpr int E = D / 32;
-    const PagedCache& c = prm.c;
-    const int b = blockIdx.y, hq = blockIdx.x, hk = hq / prm.R, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int len = paged_len(c, b);
-    auto value = [](const uint8_t* p, int e) {
-        if constexpr (INT8) return static_cast<float>(reinterpret_cast<const int8_t*>(p)[e]);
-        else return static_cast<float>(reinterpret_cast<const T*>(p)[e]);
-    };
-    constexpr int kBytes = INT8 ? 1 : 2;
-    float q[E], o[E], m = -INFINITY, z = 0.f;
-    const T* qrow = reinterpret_cast<const T*>(prm.q + b * prm.qs[0] + hq * prm.qs[1]);
-    for (int i = 0; i < E; ++i) { q[i] = static_cast<float>(qrow[lane + 32 * i]); o[i] = 0.f; }
-    for (int pos = warp; pos < len; pos += 4) {
-        const int page = paged_page(c, b, pos);
-        if (page < 0) continue;
-        const int at = pos & ((1 << c.page_shift) - 1);
-        const uint8_t* k = c.k_pool + kBytes * (page * c.ks[0] + hk * c.ks[1] + at * c.ks[2]);
-        const uint8_t* v = c.v_pool + kBytes * (page * c.vs[0] + hk * c.vs[1] + at * c.vs[2]);
-        const int64_t so = ((static_cast<int64_t>(page) * c.Hk + hk) << c.page_shift) + at;
-        float s = 0.f;
-        for (int i = 0; i < E; ++i) s += q[i] * value(k, lane + 32 * i);
-        for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-        s *= prm.scale_log2;
-        if (INT8) s *= c.k_scale[so];
-        const float m_new = fmaxf(m, s), use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = exp2f(m - use), p = exp2f(s - use);
-        z = z * alpha + p;
-        const float pv = INT8 ? p * c.v_scale[so] : p;
-        for (int i = 0; i < E; ++i) o[i] = o[i] * alpha + pv * value(v, lane + 32 * i);
-        m = m_new;
+template <class T, int D, bool INT8, int NB>
+struct Cfg {
+    static constexpr int kElt = INT8 ? 1 : 2;
+    static constexpr int CH = kStageBytes / (2 * D * kElt);         // keys of a chunk
+    static constexpr int MB = CH / 16;                              // blocks of 16 keys
+    static constexpr int kUnit = CH * kWarps;
+    static constexpr int kVOff = CH * D * kElt;                     // values behind the keys of a stage
+    static constexpr int kBoxCols = INT8 ? 1 : D / 64;              // boxes side by side in a row of 16-bit values
+    static constexpr int kFrag = (D / 16) * NB * 32;                // float4 fragments of a row's O
+    // The probabilities are carried 2^14 times as large in FP16, so that what the rounding loses is below 2^-28 of the
+    // largest instead of 2^-14.  bfloat16 has FP32's exponents.
+    static constexpr bool kHalfP = INT8 || std::is_same<T, __half>::value;
+    static constexpr float kOff = kHalfP ? 14.f : 0.f;
+    static constexpr float kUnOff = kHalfP ? 6.103515625e-5f : 1.f;
+    static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
+};
+
+// ---------------------------------------------------------------------------------------------------- warp-level pieces
+template <bool BF16>
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+template <bool TRANS>
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+    if constexpr (TRANS)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+// Bytes 0, 1 (HI = false) or 2, 3 of a word of codes + 128 as an FP16 pair.
+template <bool HI>
+__device__ __forceinline__ uint32_t codes_to_half2(uint32_t biased) {
+    const uint32_t m = __byte_perm(biased, 0x64646464u, HI ? 0x4342u : 0x4140u);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&m), __floats2half2_rn(1152.f, 1152.f));
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Key of a block of eight that row r of an INT8 fragment holds.
+template <int D>
+__device__ __forceinline__ constexpr int key_of_row(int r) {
+    return D == 128 ? ((r & 1) ? r ^ 4 : r) : r ^ ((r >> 1) & 1);
+}
+// Byte offset of the 16-byte piece `piece` of a row of codes, as the TMA swizzle places it (128- or 64-byte rows).
+template <int D>
+__device__ __forceinline__ uint32_t code_piece(int row, int piece) {
+    return D == 128 ? row * 128 + ((piece ^ (row & 7)) << 4) : row * 64 + ((piece ^ ((row >> 1) & 3)) << 4);
+}
+// ... of a row of 16-bit values: pieces 0-7 and 8-15 are boxes of their own, CH rows of 128 bytes.
+template <int CH>
+__device__ __forceinline__ uint32_t value_piece(int row, int piece) {
+    return (piece >> 3) * (CH * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+}
+
+// ---------------------------------------------------------------------------------------------------- the work list
+// Place in the list of units: rows (b, h) of n_units units, h = KV head * groups + group of query heads.
+struct Cursor {
+    int b, h, unit, n_units, len, left;      // left: units from here to the end of the CTA's run
+};
+__device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm, int unit_keys) {
+    c.unit = 0;
+    if (++c.h == prm.HG) {
+        c.h = 0;
+        do {
+            if (++c.b >= prm.c.B) {          // (only if a length changed meanwhile)
+                c.left = 0;
+                return;
+            }
+            c.len = paged_len(prm.c, c.b);
+            c.n_units = (c.len + unit_keys - 1) / unit_keys;
+        } while (c.n_units == 0);
     }
-    __shared__ float ms[4], zs[4], os[4][D];
-    for (int i = 0; i < E; ++i) os[warp][lane + 32 * i] = o[i];
-    if (lane == 0) { ms[warp] = m; zs[warp] = z; }
+}
+__device__ __forceinline__ void next_unit(Cursor& c, const PagedDecodeParams& prm, int unit_keys) {
+    --c.left;
+    if (++c.unit == c.n_units && c.left > 0) next_row(c, prm, unit_keys);
+}
+
+// The run of CTA `cta` of `ctas`: [cta U / n, (cta + 1) U / n) of the U units, n = min(ctas, U).  Whole warps, every one alike.
+__device__ __forceinline__ Cursor find_run(const PagedDecodeParams& prm, int unit_keys, int cta, int ctas, int* total, int* used) {
+    const int lane = threadIdx.x & 31, B = prm.c.B;
+    auto units_of = [&](int b) { return b < B ? (paged_len(prm.c, b) + unit_keys - 1) / unit_keys : 0; };
+    int sum = 0;
+    for (int b = lane; b < B; b += 32) sum += units_of(b);
+    const int U = __reduce_add_sync(0xffffffffu, sum) * prm.HG, n = min(ctas, U);
+    *total = U; *used = n;
+    Cursor c{};
+    if (cta >= n) return c;
+    const int first = static_cast<int>(static_cast<int64_t>(cta) * U / n);
+    c.left = static_cast<int>(static_cast<int64_t>(cta + 1) * U / n) - first;
+    int before = 0;                          // units of the sequences before the 32 in hand
+    for (int b0 = 0; b0 < B; b0 += 32) {
+        const int mine = units_of(b0 + lane) * prm.HG;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, before + upto > first);
+        if (past != 0u) {
+            const int l = __ffs(past) - 1;
+            c.b = b0 + l;
+            c.n_units = __shfl_sync(0xffffffffu, mine, l) / prm.HG;
+            const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - c.n_units * prm.HG);
+            c.h = at / c.n_units;
+            c.unit = at - c.h * c.n_units;
+            c.len = paged_len(prm.c, c.b);
+            return c;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    c.left = 0;
+    return c;
+}
+
+// ---------------------------------------------------------------------------------------------------- results
+// Fragment (md, lane) of O^T: x, y = row d0 of query columns 2 t, 2 t + 1; z, w = row d1; (d0, d1) = (16 md + g, + 8), of an
+// INT8 cache (D / 8 g + 2 md, + 1).
+__device__ __forceinline__ uint8_t* out_row(const PagedDecodeParams& prm, int b, int h, int width, int n) {
+    const int hk = h / prm.groups, first = (h - hk * prm.groups) * width;
+    return first + n < prm.R ? prm.out + b * prm.os[0] + (static_cast<int64_t>(hk) * prm.R + first + n) * prm.os[1] : nullptr;
+}
+
+// Writes the normalised fragment of query columns 2 t, 2 t + 1 of block nb, and the row's lse with fragment 0.
+template <class T, int D, bool INT8, int NB>
+__device__ __forceinline__ void write_out(const PagedDecodeParams& prm, int b, int h, int md, int nb, int lane, const float4& o,
+                                          const float (&m)[2], const float (&z)[2]) {
+    const int g = lane >> 2, t = lane & 3;
+    const float v[2][2] = {{o.x, o.z}, {o.y, o.w}};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int n = 8 * nb + 2 * t + i;
+        uint8_t* dst = out_row(prm, b, h, 8 * NB, n);
+        if (dst == nullptr) continue;
+        const bool empty = z[i] == 0.f;
+        const uint32_t two = act_pack2(empty ? 0.f : v[i][0] / z[i], empty ? 0.f : v[i][1] / z[i], T());
+        if constexpr (INT8) {
+            reinterpret_cast<uint32_t*>(dst)[(D / 16) * g + md] = two;
+        } else {
+            reinterpret_cast<uint16_t*>(dst)[16 * md + g] = static_cast<uint16_t>(two);
+            reinterpret_cast<uint16_t*>(dst)[16 * md + g + 8] = static_cast<uint16_t>(two >> 16);
+        }
+        if (md == 0 && g == 0 && prm.lse != nullptr) {
+            const int hk = h / prm.groups;
+            prm.lse[static_cast<int64_t>(b) * prm.Hq + hk * prm.R + (h - hk * prm.groups) * 8 * NB + n] =
+                empty ? -INFINITY : (m[i] + log2f(z[i])) * kLn2;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- the step
+template <class T, int D, bool INT8, int NB>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using C = Cfg<T, D, INT8, NB>;
+    constexpr int CH = C::CH, MB = C::MB;
+    constexpr bool BF16 = !C::kHalfP;
+    extern __shared__ uint8_t smem[];
+    __shared__ __align__(8) uint64_t full_bar[kWarps][kStages];
+    __shared__ int page_s[kWarps][kStages][kMaxBoxes];               // pages of the chunk in a stage; -1: a hole
+    __shared__ float m_s[kWarps][8 * NB], z_s[kWarps][8 * NB], v_ref_s[kWarps];
+    __shared__ int held_s[kWarps];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    uint8_t* ring = smem + ((1024u - (ptx::smem_u32(smem) & 1023u)) & 1023u);      // (the swizzle's pattern repeats every 1 KB)
+    const PagedCache& c = prm.c;
+    const int page_mask = (1 << c.page_shift) - 1;
+    constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
+    const int box_shift = min(c.page_shift, kChShift), box_rows = 1 << box_shift;
+
+    if (lane == 0) {
+        for (int s = 0; s < kStages; ++s) ptx::mbar_init(ptx::smem_u32(&full_bar[warp][s]), 1);
+        ptx::fence_mbar_init();
+        ptx::tma_prefetch_desc(&k_map);
+        ptx::tma_prefetch_desc(&v_map);
+    }
+    __syncwarp();
+    ptx::griddep_wait();                     // the cache, the lengths and the queries may be the work of the kernel before
+    ptx::griddep_launch_dependents();
+
+    int total, used;
+    const int cta = blockIdx.x;
+    Cursor cc = find_run(prm, C::kUnit, cta, gridDim.x, &total, &used);
+    // What the joining kernel finds for this CTA: the first CTA that begins inside a row joins that row.
+    if (tid == 0) {
+        int4 job = make_int4(-1, 0, 0, 0);
+        if (cc.left > 0 && cc.unit > 0) {
+            const int first = static_cast<int>(static_cast<int64_t>(cta) * total / used);
+            const int before = static_cast<int>(static_cast<int64_t>(cta - 1) * total / used);
+            if (before <= first - cc.unit) {
+                const int64_t end = static_cast<int64_t>(first) - cc.unit + cc.n_units;         // of the row
+                const int last = static_cast<int>((end * used - 1) / total);                    // CTA with the row's last unit
+                // sequence, row, the slot of the part in front, parts of this CTA and those behind it
+                job = make_int4(cc.b, cc.h, 2 * (cta - 1) + (before == first - cc.unit ? 0 : 1), last - cta + 1);
+            }
+        }
+        prm.join[cta] = job;
+    }
+    // sequences without a key
+    for (int b = cta; b < c.B; b += gridDim.x) {
+        if (paged_len(c, b) > 0) continue;
+        for (int i = tid; i < prm.Hq * (D / 8); i += kThreads) {
+            const int hq = i / (D / 8);
+            reinterpret_cast<uint4*>(prm.out + b * prm.os[0] + hq * prm.os[1])[i - hq * (D / 8)] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        if (prm.lse != nullptr)
+            for (int hq = tid; hq < prm.Hq; hq += kThreads) prm.lse[static_cast<int64_t>(b) * prm.Hq + hq] = -INFINITY;
+    }
+
+    const uint32_t ring_u32 = ptx::smem_u32(ring) + warp * (kStages * kStageBytes);
+    Cursor ic = cc;                          // of the copies, ahead of the one of the products
+    int issued = 0, taken = 0;
+    bool failed = false;                     // a wait ran out: no more copies, and the rows from here on are NaN
+    int failed_at = 0;
+
+    // Starts the copies of this warp's next chunk, if there is one, into the stage that is free.
+    auto issue = [&]() {
+        int start = 0;
+        while (ic.left > 0) {
+            start = (ic.unit * kWarps + warp) * CH;
+            if (start < ic.len) break;
+            next_unit(ic, prm, C::kUnit);
+        }
+        if (ic.left <= 0) return;
+        const int s = issued % kStages;
+        {
+            const int boxes = (min(CH, ic.len - start) + box_rows - 1) >> box_shift;
+            const uint32_t bar = ptx::smem_u32(&full_bar[warp][s]);
+            const int hk = ic.h / prm.groups;
+            int page = -1, row = 0;
+            if (lane < boxes) {
+                const int pos = start + lane * box_rows;
+                page = paged_page(c, ic.b, pos);
+                row = pos & page_mask;
+                page_s[warp][s][lane] = page;
+            }
+            const bool drop = issued == prm.drop_chunk;
+            if (lane == 0 && !drop) ptx::mbar_arrive_expect_tx(bar, boxes * box_rows * (2 * D * C::kElt));
+            __syncwarp();
+            if (lane < boxes && !drop) {
+                // (a hole's box lies outside the map: zeros arrive, nothing is read)
+                const uint32_t dst = ring_u32 + s * kStageBytes + lane * box_rows * (INT8 ? D : 128);
+#pragma unroll
+                for (int col = 0; col < C::kBoxCols; ++col) {
+                    ptx::tma_load_4d(dst + col * (CH * 128), &k_map, bar, col * 64, row, hk, page);
+                    ptx::tma_load_4d(dst + col * (CH * 128) + C::kVOff, &v_map, bar, col * 64, row, hk, page);
+                }
+            }
+        }
+        ++issued;
+        next_unit(ic, prm, C::kUnit);
+    };
+    // Bounded wait for chunk number `taken`.
+    auto landed = [&]() -> bool {
+        const uint32_t bar = ptx::smem_u32(&full_bar[warp][taken % kStages]), parity = (taken / kStages) & 1;
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+        const uint64_t begin = ptx::globaltimer_ns();
+        uint32_t spins = 0;
+        while (!ptx::mbar_try_wait(bar, parity))
+            if ((++spins & 63u) == 0u && ptx::globaltimer_ns() - begin > prm.wait_limit_ns) return false;
+        return true;
+    };
+
+#pragma unroll 1
+    for (int s = 0; s < kStages; ++s) issue();
+    __syncwarp();
+
+    bool first_segment = true;
+#pragma unroll 1
+    while (cc.left > 0) {
+        // ------------------------------------------------ a row, or this CTA's part of it
+        const int u_end = min(cc.n_units, cc.unit + cc.left);
+        const int hk = cc.h / prm.groups, q_first = (cc.h - hk * prm.groups) * 8 * NB;
+        // scales of the block's keys of rows g and g + 8 of chunk `number`, whose first key is `start`
+        float dk[MB][2], dv[MB][2];
+        auto load_scales = [&](int number, int start, float (&xk)[MB][2], float (&xv)[MB][2]) {
+            if constexpr (INT8) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    const int pos = start + 16 * mb;
+                    const int page = pos < cc.len ? page_s[warp][number % kStages][16 * mb >> box_shift] : -1;
+                    const int64_t at = ((static_cast<int64_t>(page) * c.Hk + hk) << c.page_shift) + (pos & page_mask);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int key = 8 * i + key_of_row<D>(g);
+                        const bool on = page >= 0 && pos + key < cc.len;
+                        xk[mb][i] = on ? __ldcg(c.k_scale + at + key) : 0.f;
+                        xv[mb][i] = on ? __ldcg(c.v_scale + at + key) : 0.f;
+                    }
+                }
+            }
+        };
+        int start = (cc.unit * kWarps + warp) * CH;
+        const int end = min(cc.len, u_end * C::kUnit);        // keys of this segment
+        if (start < end && !failed) load_scales(taken, start, dk, dv);
+
+        // ---- query fragments: the right operand (columns = heads g of the block), and what a score is multiplied by
+        uint32_t qf[NB][D / 16][2];
+        float q_mul[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const bool on = q_first + 8 * nb + g < prm.R;
+            const uint8_t* row = prm.q + cc.b * prm.qs[0] + (static_cast<int64_t>(hk) * prm.R + q_first + 8 * nb + g) * prm.qs[1];
+            if constexpr (INT8) {
+                // fragment 4 j + w holds features 16 (t + 4 j) + 4 w .. + 3, as the codes come
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                        if (on) x = __ldcg(reinterpret_cast<const uint4*>(row + 32 * (t + 4 * j)) + i);
+                        qf[nb][4 * j + 2 * i][0] = x.x; qf[nb][4 * j + 2 * i][1] = x.y;
+                        qf[nb][4 * j + 2 * i + 1][0] = x.z; qf[nb][4 * j + 2 * i + 1][1] = x.w;
+                    }
+                q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
+                if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                    // bfloat16 queries as FP16: multiplied by the power of two that brings the row's largest value to
+                    // [2^13, 2^14); eight mantissa bits fit, and what becomes subnormal is below 2^-27 of the largest
+                    uint32_t top = 0u;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const uint32_t a = qf[nb][i][k] & 0x7fff7fffu;
+                            top = max(top, max(a & 0xffffu, a >> 16));
+                        }
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    const uint32_t e = top == 0u ? 140u : max(top >> 7, 14u);
+                    const float up = __uint_as_float((267u - e) << 23), down = __uint_as_float((e - 13u) << 23);
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float2 f = act_to_float2(qf[nb][i][k], __nv_bfloat16());
+                            qf[nb][i][k] = act_pack2(f.x * up, f.y * up, __half());
+                        }
+                    q_mul[nb][0] *= __shfl_sync(0xffffffffu, down, 8 * t);
+                    q_mul[nb][1] *= __shfl_sync(0xffffffffu, down, 8 * t + 4);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        qf[nb][i][k] = on ? __ldcg(reinterpret_cast<const uint32_t*>(row + 32 * i + 16 * k) + t) : 0u;
+                q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
+            }
+        }
+
+        float m_run[NB][2], z[NB][2], acc[D / 16][NB][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            m_run[nb][0] = m_run[nb][1] = -INFINITY;
+            z[nb][0] = z[nb][1] = 0.f;
+#pragma unroll
+            for (int md = 0; md < D / 16; ++md) acc[md][nb][0] = acc[md][nb][1] = acc[md][nb][2] = acc[md][nb][3] = 0.f;
+        }
+        // INT8: the scale of a value is folded into its probability relative to v_ref, a power of two at or above every
+        // scale so far; O~ is in units of it.
+        float v_ref = 7.888609052210118e-31f;                 // 2^-100
+        bool any = false;
+
+#pragma unroll 1
+        for (; start < end; start += C::kUnit) {
+            any = true;
+            const bool more = start + C::kUnit < end;
+            float dk_next[MB][2], dv_next[MB][2];
+            if (more && !failed) load_scales(taken + 1, start + C::kUnit, dk_next, dv_next);
+            if (!failed && !landed()) {
+                failed = true;
+                failed_at = taken;
+            }
+            if (!failed) {
+                const int s = taken % kStages;
+                const uint32_t kst = ring_u32 + s * kStageBytes, vst = kst + C::kVOff;
+                const int live = min(CH, cc.len - start);               // keys of the chunk
+                const int blocks = (live + 15) / 16;
+                // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same)
+                float sc[MB][NB][4];
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) sc[mb][nb][0] = sc[mb][nb][1] = sc[mb][nb][2] = sc[mb][nb][3] = 0.f;
+                    if (mb < blocks) {
+                        if constexpr (INT8) {
+                            const int r0 = 16 * mb + key_of_row<D>(g);
+#pragma unroll
+                            for (int j = 0; j < D / 64; ++j) {
+                                const uint4 xa = lds128(kst + code_piece<D>(r0, t + 4 * j)), xb = lds128(kst + code_piece<D>(r0 + 8, t + 4 * j));
+                                const uint32_t wa[4] = {xa.x, xa.y, xa.z, xa.w}, wb[4] = {xb.x, xb.y, xb.z, xb.w};
+#pragma unroll
+                                for (int w = 0; w < 4; ++w) {
+                                    const uint32_t ua = wa[w] ^ 0x80808080u, ub = wb[w] ^ 0x80808080u;
+                                    const uint32_t a0 = codes_to_half2<false>(ua), a2 = codes_to_half2<true>(ua);
+                                    const uint32_t a1 = codes_to_half2<false>(ub), a3 = codes_to_half2<true>(ub);
+#pragma unroll
+                                    for (int nb = 0; nb < NB; ++nb)
+                                        mma_16816<false>(sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
+                                }
+                            }
+                        } else {
+                            const int row = 16 * mb + (lane & 15), piece = lane >> 4;
+#pragma unroll
+                            for (int i = 0; i < D / 16; ++i) {
+                                uint32_t a[4];
+                                ldmatrix_x4<false>(a, kst + value_piece<CH>(row, 2 * i + piece));
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
+                            }
+                        }
+                    }
+                }
+                // ---- scales; keys past the end and in holes do not exist
+                uint32_t dv_top = 0u;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    const bool hole = mb < blocks && page_s[warp][s][16 * mb >> box_shift] < 0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int key = 16 * mb + 8 * i + (INT8 ? key_of_row<D>(g) : g);
+                        const bool on = key < live && !hole;
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                float x = sc[mb][nb][2 * i + k];
+                                if constexpr (INT8) x *= dk[mb][i];
+                                sc[mb][nb][2 * i + k] = on ? x : -INFINITY;
+                            }
+                        if constexpr (INT8) dv_top = max(dv_top, __float_as_uint(dv[mb][i]) & 0x7fffffffu);
+                    }
+                }
+                // ---- running maximum, over the lanes of a column; alpha brings what has been summed to the new one
+                float sub[NB][2], alpha[NB][2];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float top = fmaxf(sc[0][nb][k], sc[0][nb][2 + k]);
+#pragma unroll
+                        for (int mb = 1; mb < MB; ++mb) top = fmax3(top, sc[mb][nb][k], sc[mb][nb][2 + k]);
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                        const float m_new = fmaxf(m_run[nb][k], top * q_mul[nb][k]);
+                        const float m_use = m_new == -INFINITY ? 0.f : m_new;      // (nothing but holes so far)
+                        alpha[nb][k] = exp2f(m_run[nb][k] - m_use);
+                        sub[nb][k] = C::kOff - m_use;
+                        m_run[nb][k] = m_new;
+                        z[nb][k] *= alpha[nb][k];
+                    }
+                float v_mul[MB][2];
+                if constexpr (INT8) {
+                    dv_top = __reduce_max_sync(0xffffffffu, dv_top);
+                    const uint32_t want = (min(dv_top, 0x7e800000u) + 0x7fffffu) & 0x7f800000u, have = __float_as_uint(v_ref);
+                    if (want > have) {          // (the same in the whole warp)
+                        const float back = __uint_as_float(have) * __uint_as_float(0x7f000000u - want);
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) { alpha[nb][0] *= back; alpha[nb][1] *= back; }
+                        v_ref = __uint_as_float(want);
+                    }
+                    const float inv = __uint_as_float(0x7f000000u - __float_as_uint(v_ref));
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) { v_mul[mb][0] = dv[mb][0] * inv; v_mul[mb][1] = dv[mb][1] * inv; }
+                }
+                bool still = true;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) still = still && alpha[nb][0] == 1.f && alpha[nb][1] == 1.f;
+                if (!__all_sync(0xffffffffu, still)) {
+#pragma unroll
+                    for (int md = 0; md < D / 16; ++md)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            acc[md][nb][0] *= alpha[nb][0]; acc[md][nb][1] *= alpha[nb][1];
+                            acc[md][nb][2] *= alpha[nb][0]; acc[md][nb][3] *= alpha[nb][1];
+                        }
+                }
+                // ---- probabilities, and O^T += V^T P^T block by block
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    if (mb >= blocks) continue;
+                    uint32_t p0[NB], p1[NB];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        float p[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            p[k] = fast_exp2(fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]));
+                            z[nb][k & 1] += p[k];
+                            if constexpr (INT8) p[k] *= v_mul[mb][k >> 1];
+                        }
+                        using P = typename std::conditional<C::kHalfP, __half, __nv_bfloat16>::type;
+                        p0[nb] = transpose_8x8(act_pack2(p[0], p[1], P()));
+                        p1[nb] = transpose_8x8(act_pack2(p[2], p[3], P()));
+                    }
+                    if constexpr (INT8) {
+                        // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
+                        const int r0 = 16 * mb + key_of_row<D>(2 * t), r1 = 16 * mb + key_of_row<D>(2 * t + 1);
+                        uint32_t x[4][D / 32];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int row = (i & 1 ? r1 : r0) + (i >> 1) * 8;
+                            if constexpr (D == 128) {
+                                const uint4 v = lds128(vst + code_piece<D>(row, g));
+                                x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+                            } else {
+                                const uint2 v = lds64(vst + code_piece<D>(row, g >> 1) + 8 * (g & 1));
+                                x[i][0] = v.x; x[i][1] = v.y;
+                            }
+                        }
+#pragma unroll
+                        for (int w = 0; w < D / 32; ++w) {
+                            const uint32_t u0 = x[0][w] ^ 0x80808080u, u1 = x[1][w] ^ 0x80808080u;
+                            const uint32_t u2 = x[2][w] ^ 0x80808080u, u3 = x[3][w] ^ 0x80808080u;
+                            const uint32_t lo01 = __byte_perm(u0, u1, 0x5140), hi01 = __byte_perm(u0, u1, 0x7362);
+                            const uint32_t lo23 = __byte_perm(u2, u3, 0x5140), hi23 = __byte_perm(u2, u3, 0x7362);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t a01 = e ? hi01 : lo01, a23 = e ? hi23 : lo23;
+                                const uint32_t a0 = codes_to_half2<false>(a01), a1 = codes_to_half2<true>(a01);
+                                const uint32_t a2 = codes_to_half2<false>(a23), a3 = codes_to_half2<true>(a23);
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb) mma_16816<false>(acc[2 * w + e][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
+                            }
+                        }
+                    } else {
+                        // (what lies behind the last key may be anything, and 0 times a NaN is one)
+                        const bool cut = 16 * mb + 16 > live;
+                        uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+                        if (cut) {
+                            const int k0 = 16 * mb + 2 * t;
+                            keep0 = (k0 < live ? 0xffffu : 0u) | (k0 + 1 < live ? 0xffff0000u : 0u);
+                            keep1 = (k0 + 8 < live ? 0xffffu : 0u) | (k0 + 9 < live ? 0xffff0000u : 0u);
+                        }
+                        const int row = 16 * mb + (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1;
+#pragma unroll
+                        for (int md = 0; md < D / 16; ++md) {
+                            uint32_t a[4];
+                            ldmatrix_x4<true>(a, vst + value_piece<CH>(row, 2 * md + piece));
+                            a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
+                        }
+                    }
+                }
+            }
+            ++taken;
+            __syncwarp();                    // every lane is done with the stage
+            if (more) {
+                if (!failed) issue();
+                __syncwarp();
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    dk[mb][0] = dk_next[mb][0]; dk[mb][1] = dk_next[mb][1];
+                    dv[mb][0] = dv_next[mb][0]; dv[mb][1] = dv_next[mb][1];
+                }
+            }
+        }
+
+        // ------------------------------------------------ the warps' results of the segment, merged in the stages read last
+        // (a warp's last stage of a segment is refilled after the merge; every warp holds the same places of O^T)
+        if (failed)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) z[nb][0] = z[nb][1] = NAN;
+        const int held = (taken + kStages - 1) % kStages;           // of chunk taken - 1
+        float4* mine = reinterpret_cast<float4*>(ring + (warp * kStages + held) * kStageBytes);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 4);
+                z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 8);
+                z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 16);
+                if (g == 0) { m_s[warp][8 * nb + 2 * t + k] = m_run[nb][k]; z_s[warp][8 * nb + 2 * t + k] = z[nb][k]; }
+            }
+            if (any && !failed)
+#pragma unroll
+                for (int md = 0; md < D / 16; ++md)
+                    mine[(md * NB + nb) * 32 + lane] = make_float4(acc[md][nb][0], acc[md][nb][1], acc[md][nb][2], acc[md][nb][3]);
+        }
+        // (a warp without a chunk of the segment has no stage to itself: weight 0, and its place is not read)
+        if (lane == 0) {
+            v_ref_s[warp] = any && !failed ? (INT8 ? v_ref : 1.f) : -1.f;
+            held_s[warp] = held;
+        }
+        __syncthreads();
+        {
+            const bool whole = cc.unit == 0 && u_end == cc.n_units;
+            const int slot = 2 * cta + (first_segment ? 0 : 1);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float m[2], zz[2], wgt[kWarps][2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int n = 8 * nb + 2 * t + k;
+                    m[k] = fmaxf(fmaxf(m_s[0][n], m_s[1][n]), fmaxf(m_s[2][n], m_s[3][n]));
+                    const float use = m[k] == -INFINITY ? 0.f : m[k];
+                    zz[k] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float f = exp2f(m_s[w][n] - use) * C::kUnOff;
+                        zz[k] += z_s[w][n] * f;
+                        wgt[w][k] = f * v_ref_s[w];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16 / kWarps; ++i) {
+                    const int md = warp + kWarps * i;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        if (v_ref_s[w] < 0.f) continue;
+                        const float4 x = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes)[(md * NB + nb) * 32 + lane];
+                        o.x += x.x * wgt[w][0]; o.y += x.y * wgt[w][1]; o.z += x.z * wgt[w][0]; o.w += x.w * wgt[w][1];
+                    }
+                    if (whole) write_out<T, D, INT8, NB>(prm, cc.b, cc.h, md, nb, lane, o, m, zz);
+                    else prm.part_o[(static_cast<int64_t>(slot) * (D / 16) + md) * (NB * 32) + nb * 32 + lane] = o;
+                }
+                if (!whole && warp == 0 && g == 0) {
+                    prm.part_mz[slot * (8 * NB) + 8 * nb + 2 * t] = make_float2(m[0], zz[0]);
+                    prm.part_mz[slot * (8 * NB) + 8 * nb + 2 * t + 1] = make_float2(m[1], zz[1]);
+                }
+            }
+        }
+        ptx::fence_proxy_async_smem();       // the stages go back to the copies
+        __syncthreads();
+        if (any && !failed) issue();
+        __syncwarp();
+        first_segment = false;
+        cc.left -= u_end - cc.unit;
+        if (cc.left > 0) next_row(cc, prm, C::kUnit);
+    }
+
+    if (failed) {
+        // the copies that are still on the way land before the shared memory is given back
+        for (int i = failed_at; i < issued; ++i) {
+            if (i == prm.drop_chunk) continue;
+            for (int spin = 0; spin < (1 << 16); ++spin)
+                if (ptx::mbar_try_wait(ptx::smem_u32(&full_bar[warp][i % kStages]), (i / kStages) & 1)) break;
+        }
+    }
+}
+
+// Joins the parts of a row that several CTAs shared: job (b, h, s, n) of the CTA blockIdx.x names slot s and, of that CTA and
+// the n - 1 behind it, their first slots.  Block y takes rows md = y of the fragments; its warps take the parts in turn and
+// several at a time (what bounds it is the round trips), then merge in shared memory.
+constexpr int kJoinWarps = 8, kJoinAtOnce = 4;
+template <class T, int D, bool INT8, int NB>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+paged_join_kernel(const PagedDecodeParams prm) {
+    __shared__ float4 o_s[kJoinWarps][NB][32];
+    __shared__ float2 mz_s[kJoinWarps][NB][32][2];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int4 job = __ldcg(prm.join + blockIdx.x);
+    if (job.x < 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, md = blockIdx.y, parts = job.w + 1;
+    float4 o[NB];
+    float m[NB][2], z[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        o[nb] = make_float4(0.f, 0.f, 0.f, 0.f);
+        m[nb][0] = m[nb][1] = -INFINITY;
+        z[nb][0] = z[nb][1] = 0.f;
+    }
+    auto add = [&](int nb, const float4& x, const float2 (&mz)[2]) {
+        float back[2], fore[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float top = fmaxf(m[nb][k], mz[k].x), use = top == -INFINITY ? 0.f : top;
+            back[k] = exp2f(m[nb][k] - use);
+            fore[k] = exp2f(mz[k].x - use);
+            z[nb][k] = z[nb][k] * back[k] + mz[k].y * fore[k];
+            m[nb][k] = top;
+        }
+        o[nb].x = o[nb].x * back[0] + x.x * fore[0]; o[nb].y = o[nb].y * back[1] + x.y * fore[1];
+        o[nb].z = o[nb].z * back[0] + x.z * fore[0]; o[nb].w = o[nb].w * back[1] + x.w * fore[1];
+    };
+    for (int i0 = warp; i0 < parts; i0 += kJoinWarps * kJoinAtOnce) {
+        float4 x[kJoinAtOnce][NB];
+        float2 mz[kJoinAtOnce][NB][2];
+#pragma unroll
+        for (int j = 0; j < kJoinAtOnce; ++j) {
+            const int i = i0 + j * kJoinWarps;
+            if (i >= parts) continue;
+            const int64_t slot = i == 0 ? job.z : 2 * (static_cast<int>(blockIdx.x) + i - 1);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                x[j][nb] = __ldcg(prm.part_o + (slot * (D / 16) + md) * (NB * 32) + nb * 32 + lane);
+                const float4 two = __ldcg(reinterpret_cast<const float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t));
+                mz[j][nb][0] = make_float2(two.x, two.y);
+                mz[j][nb][1] = make_float2(two.z, two.w);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kJoinAtOnce; ++j)
+            if (i0 + j * kJoinWarps < parts)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) add(nb, x[j][nb], mz[j][nb]);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        o_s[warp][nb][lane] = o[nb];
+        mz_s[warp][nb][lane][0] = make_float2(m[nb][0], z[nb][0]);
+        mz_s[warp][nb][lane][1] = make_float2(m[nb][1], z[nb][1]);
+    }
     __syncthreads();
-    if (threadIdx.x >= D) return;
-    m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-    const float use = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
-    z = 0.f;
-    for (int w = 0; w < 4; ++w) { const float a = exp2f(ms[w] - use); z += zs[w] * a; sum += os[w][threadIdx.x] * a; }
-    reinterpret_cast<T*>(prm.out + b * prm.os[0] + hq * prm.os[1])[threadIdx.x] = static_cast<T>(z == 0.f ? 0.f : sum / z);
-    if (threadIdx.x == 0 && prm.lse != nullptr) prm.lse[static_cast<int64_t>(b) * prm.Hq + hq] = z == 0.f ? -INFINITY : (m + log2f(z)) * kLn2;
+    if (warp >= NB) return;
+    const int nb = warp;
+    o[0] = o_s[0][nb][lane];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) { m[0][k] = mz_s[0][nb][lane][k].x; z[0][k] = mz_s[0][nb][lane][k].y; }
+    for (int w = 1; w < min(kJoinWarps, parts); ++w) add(0, o_s[w][nb][lane], mz_s[w][nb][lane]);
+    write_out<T, D, INT8, NB>(prm, job.x, job.y, md, nb, lane, o[0], m[0], z[0]);
 }
 
-using DecodeKernel = void (*)(const PagedDecodeParams);
+// ---------------------------------------------------------------------------------------------------- host
 
-template <class T>
-DecodeKernel pick(int d, bool int8) {
-    if (d == 128) return int8 ? paged_decode_kernel<T, 128, true> : paged_decode_kernel<T, 128, false>;
-    return int8 ? paged_decode_kernel<T, 64, true> : paged_decode_kernel<T, 64, false>;
-}
+struct Plan {
+    int NB, groups, HG, unit, ctas, splits;      // splits: whether a row can have more units than one
+    size_t join_bytes, mz_bytes, total;
+};
 
-constexpr size_t kWorkspace = 256;
-
-int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c) {
+int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* plan) {
     const int rc = resolve_paged(p, c);
     if (rc) return rc;
-    if (heads_q <= 0 || heads_q % p->heads_kv != 0 || p->batch > 65535) return TILEMIX_ERR_SHAPE;
+    if (heads_q <= 0 || heads_q % p->heads_kv != 0) return TILEMIX_ERR_SHAPE;
+    const int R = heads_q / p->heads_kv;
+    plan->NB = R > 8 ? 2 : 1;
+    plan->groups = static_cast<int>(ceil_div(R, 8 * plan->NB));
+    const int elt = p->cache_type == TILEMIX_CACHE_INT8 ? 1 : 2;
+    plan->unit = kWarps * kStageBytes / (2 * p->head_dim * elt);
+    const int64_t rows = static_cast<int64_t>(p->heads_kv) * plan->groups;
+    const int64_t units = rows * p->batch * ceil_div(c->capacity, plan->unit);
+    if (rows > (1 << 24) || units > (int64_t{1} << 30) || static_cast<int64_t>(p->batch) * heads_q > (int64_t{1} << 30)) return TILEMIX_ERR_SHAPE;
+    plan->HG = static_cast<int>(rows);
+    plan->ctas = static_cast<int>(units < kCtasPerSm * kSms ? units : kCtasPerSm * kSms);
+    plan->splits = c->capacity > plan->unit;
+    plan->join_bytes = (plan->ctas * sizeof(int4) + 255) / 256 * 256;
+    plan->mz_bytes = (static_cast<size_t>(plan->ctas) * 2 * 8 * plan->NB * sizeof(float2) + 255) / 256 * 256;
+    plan->total = plan->join_bytes + plan->mz_bytes + static_cast<size_t>(plan->ctas) * 2 * p->head_dim * 8 * plan->NB * sizeof(float);
     return TILEMIX_OK;
 }
 
@@ -91,11 +827,50 @@ int row_strides(const int64_t* in, int B, int H, int d, bool output, int64_t out
     const int64_t size[2] = {B, H}, dense[2] = {static_cast<int64_t>(H) * d, d};
     for (int i = 0; i < 2; ++i) {
         const int64_t s = in != nullptr ? in[i] : dense[i];
-        if (s < 0 || s > (int64_t{1} << 40) || (output && size[i] > 1 && s < d)) return TILEMIX_ERR_SHAPE;
+        if (size[i] > 1 && (s < 0 || s > (int64_t{1} << 40) || (output && s < d))) return TILEMIX_ERR_SHAPE;
         if (size[i] > 1 && s * 2 % 16 != 0) return TILEMIX_ERR_ALIGN;
         out[i] = size[i] == 1 ? 0 : 2 * s;
     }
+    if (output && B > 1 && H > 1) {       // rows that overlap
+        const int64_t a = out[0] < out[1] ? out[0] : out[1], z = out[0] < out[1] ? out[1] : out[0];
+        const int64_t n = out[0] < out[1] ? B : H;
+        if (z < a * (n - 1) + 2 * d) return TILEMIX_ERR_SHAPE;
+    }
     return TILEMIX_OK;
+}
+
+template <class T, int D, bool INT8, int NB>
+int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) {
+    using C = Cfg<T, D, INT8, NB>;
+    const PagedCache& c = prm.c;
+    CUtensorMap km, vm;
+    const int page = 1 << c.page_shift, box_rows = page < C::CH ? page : C::CH;
+    int rc;
+    if ((rc = encode_pool_map(&km, c.k_pool, C::kElt, D, page, c.Hk, c.n_pages, c.ks, box_rows))) return rc;
+    if ((rc = encode_pool_map(&vm, c.v_pool, C::kElt, D, page, c.Hk, c.n_pages, c.vs, box_rows))) return rc;
+    auto kernel = paged_decode_kernel<T, D, INT8, NB>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return static_cast<int>(e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(plan.ctas); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, prm, km, vm);
+    g_launch_count.fetch_add(1);
+    if (e != cudaSuccess || !plan.splits) return static_cast<int>(e);
+    cfg.gridDim = dim3(plan.ctas, D / 16); cfg.blockDim = dim3(32 * kJoinWarps); cfg.dynamicSmemBytes = 0;
+    e = cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB>, prm);
+    g_launch_count.fetch_add(1);
+    return static_cast<int>(e);
+}
+
+using Launch = int (*)(const PagedDecodeParams&, const Plan&, cudaStream_t);
+template <class T, int D>
+Launch pick(bool int8, int NB) {
+    if (int8) return NB == 1 ? launch<T, D, true, 1> : launch<T, D, true, 2>;
+    return NB == 1 ? launch<T, D, false, 1> : launch<T, D, false, 2>;
 }
 
 }  // namespace
@@ -107,30 +882,38 @@ extern "C" {
 
 size_t tilemix_paged_decode_workspace_size(const tilemix_paged_t* p, int32_t heads_q) {
     PagedCache c;
-    return resolve_decode(p, heads_q, &c) ? 0 : kWorkspace;
+    Plan plan;
+    return resolve_decode(p, heads_q, &c, &plan) ? 0 : plan.total;
 }
 
 int tilemix_paged_decode(const tilemix_paged_t* p, int32_t heads_q, float softmax_scale, const void* q, const int64_t* q_stride,
                          void* out, const int64_t* out_stride, float* lse, void* workspace, size_t workspace_bytes,
                          void* stream) {
     PagedDecodeParams prm{};
-    int rc = resolve_decode(p, heads_q, &prm.c);
+    Plan plan;
+    int rc = resolve_decode(p, heads_q, &prm.c, &plan);
     if (rc) return rc;
     if (!q || !out || !workspace) return TILEMIX_ERR_NULL;
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return TILEMIX_ERR_ALIGN;
     if ((rc = row_strides(q_stride, p->batch, heads_q, p->head_dim, false, prm.qs))) return rc;
     if ((rc = row_strides(out_stride, p->batch, heads_q, p->head_dim, true, prm.os))) return rc;
-    if (workspace_bytes < kWorkspace) return TILEMIX_ERR_WORKSPACE;
-    prm.Hq = heads_q; prm.R = heads_q / p->heads_kv;
+    if (workspace_bytes < plan.total) return TILEMIX_ERR_WORKSPACE;
+    prm.Hq = heads_q; prm.R = heads_q / p->heads_kv; prm.groups = plan.groups; prm.HG = plan.HG;
     prm.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(p->head_dim))) * kLog2e;
     prm.q = static_cast<const uint8_t*>(q);
     prm.out = static_cast<uint8_t*>(out);
     prm.lse = lse;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    prm.join = reinterpret_cast<int4*>(ws);
+    prm.part_mz = reinterpret_cast<float2*>(ws + plan.join_bytes);
+    prm.part_o = reinterpret_cast<float4*>(ws + plan.join_bytes + plan.mz_bytes);
+    prm.wait_limit_ns = g_wait_limit_ns.load();
+    prm.drop_chunk = g_test_drop.load() == 2 ? 1 : -1;
     const bool int8 = p->cache_type == TILEMIX_CACHE_INT8;
-    const DecodeKernel kernel = p->act_type == TILEMIX_TYPE_FP16 ? pick<__half>(p->head_dim, int8) : pick<__nv_bfloat16>(p->head_dim, int8);
-    kernel<<<dim3(heads_q, p->batch), 128, 0, static_cast<cudaStream_t>(stream)>>>(prm);
-    g_launch_count.fetch_add(1);
-    return static_cast<int>(cudaGetLastError());
+    Launch go;
+    if (p->act_type == TILEMIX_TYPE_FP16) go = p->head_dim == 128 ? pick<__half, 128>(int8, plan.NB) : pick<__half, 64>(int8, plan.NB);
+    else go = p->head_dim == 128 ? pick<__nv_bfloat16, 128>(int8, plan.NB) : pick<__nv_bfloat16, 64>(int8, plan.NB);
+    return go(prm, plan, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -340,6 +340,30 @@ def test_decode_workspace_may_hold_anything():
         assert (guard[size:] == 77).all()
 
 
+@pytest.mark.parametrize("act,int8,hq", [("fp16", True, 8), ("bf16", False, 8), ("bf16", True, 128)])
+def test_bounded_waits(act, int8, hq):
+    """A copy that never lands: the wait runs out, the call returns, the rows that a warp had still to work on are NaN, the
+    others as ever, and the context and the next call are in order."""
+    t = tm()
+    s = ref.Setup(act, int8, 64, 16, 8, [10, 40000, 12], seed=3, device=DEV)
+    q = query(s, hq)
+    c = s.cache()
+    good = t.tilemix_paged_decode(c, q, want_lse=True)
+    torch.cuda.synchronize()
+    t.tilemix_test_drop_copy(2, 20_000_000)
+    try:
+        res = t.tilemix_paged_decode(c, q, want_lse=True)
+        torch.cuda.synchronize()
+    finally:
+        t.tilemix_test_drop_copy(0)
+    assert torch.isnan(res["out"][1]).all() and torch.isnan(res["lse"][1]).all()
+    whole = ~torch.isnan(res["lse"])
+    assert whole[0, 0] and torch.equal(res["out"][whole], good["out"][whole]) and torch.isnan(res["out"][~whole]).all()
+    again = t.tilemix_paged_decode(c, q, want_lse=True)
+    assert torch.equal(again["out"], good["out"]) and torch.equal(again["lse"], good["lse"])
+    ref.check_decode(s, q, again)
+
+
 # ---------------------------------------------------------------------------------------------------- together
 
 @pytest.mark.parametrize("act,int8", KINDS)
