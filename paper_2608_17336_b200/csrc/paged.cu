@@ -62,7 +62,7 @@ int resolve_paged(const tilemix_paged_t* p, PagedCache* c) {
     if ((rc = checked_strides(all_zero3(p->v_stride) ? dense : p->v_stride, size, 3, p->head_dim, int8 ? 1 : 2, c->vs))) return rc;
     if (!p->k_pool || !p->v_pool || !p->block_table || !p->cache_len || (int8 && (!p->k_scale || !p->v_scale))) return TILEMIX_ERR_NULL;
     if (!aligned16(p->k_pool) || !aligned16(p->v_pool) || !aligned4(p->block_table) || !aligned4(p->cache_len) ||
-        (int8 && (!aligned4(p->k_scale) || !aligned4(p->v_scale))))
+        (int8 && (!aligned16(p->k_scale) || !aligned16(p->v_scale))))
         return TILEMIX_ERR_ALIGN;
     c->k_pool = static_cast<uint8_t*>(p->k_pool); c->v_pool = static_cast<uint8_t*>(p->v_pool);
     c->k_scale = int8 ? p->k_scale : nullptr; c->v_scale = int8 ? p->v_scale : nullptr;

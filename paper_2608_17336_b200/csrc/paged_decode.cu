@@ -5,13 +5,14 @@
 // warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
 // at the cost of ~17 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.
 //
-// Layout of the work.  A warp owns a ring of three 8 KB stages and takes CHUNKS of 16 to 64 keys (4 KB of keys, 4 KB of values),
-// which one TMA box a page brings in, swizzled; no warp waits for another but at the end of a row.  Four warps are a CTA,
-// two CTAs share an SM: 192 KB on the way.  Four neighbouring chunks are a UNIT; the units of all (sequence, KV head) rows,
-// one row behind the other, are dealt out to the CTAs in equal runs, so that a batch of unequal lengths keeps every SM busy to
-// the end.  A CTA finds its run from the lengths, which only the device knows.  Rows inside its run it finishes itself; of
-// a row that it shares with its neighbours it leaves a partial result (m, z, O) to the joining kernel.  The ring runs
-// on across rows.
+// Layout of the work.  A CTA has four or eight warps at the products and one that starts the copies; two CTAs share an SM.
+// Every warp of the first kind owns a ring of three stages and takes CHUNKS of 16 to 64 keys out of it, which one TMA box a
+// page brings in, swizzled (with the scales, where there are any): 192 KB of an SM's shared memory are on the way, and no warp
+// waits for another but at the end of a row.  Neighbouring chunks, one for each warp, are a UNIT; the units of all
+// (sequence, KV head) rows, one row behind the other, are dealt out to the CTAs in equal runs, so that a batch of unequal
+// lengths keeps every SM busy to the end.  A CTA finds its run from the lengths, which only the device knows.  Rows inside
+// its run it finishes itself; of a row that it shares with its neighbours it leaves a partial result (m, z, O) to the joining
+// kernel.  The copies run on across rows.
 //
 // Products.  S^T = K Q^T with the KEYS as the 16 rows of the MMA and eight query heads as its columns, then O^T = V^T P^T with
 // the head dimension as the rows: nothing of a 16-row operand is wasted on absent query heads, and O^T takes D / 32 * 8
@@ -36,10 +37,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kStages = 3, kStageBytes = 8192, kRingBytes = kWarps * kStages * kStageBytes, kSmemBytes = kRingBytes + 1024;
+constexpr int kStages = 3, kRingBytes = 96 * 1024;
 constexpr int kCtasPerSm = 2, kSms = 148;
-constexpr int kMaxBoxes = 4;            // pages of a chunk: at most 64 keys in pages of 16
 
 struct PagedDecodeParams {
     PagedCache c;
@@ -60,19 +59,31 @@ struct PagedDecodeParams {
 template <class T, int D, bool INT8, int NB>
 struct Cfg {
     static constexpr int kElt = INT8 ? 1 : 2;
+    // Warps at the products.  The INT8 form is bound by issue slots and latencies, not by bytes, unless many warps share them
+    // (8 x 32K keys, d = 128: four a CTA 135 us, eight XX us); sixteen query heads need the registers of four.
+    static constexpr int W = INT8 && NB == 1 ? 8 : 4;
+    static constexpr int kThreads = 32 * (W + 1);
+    static constexpr int kStageBytes = kRingBytes / (W * kStages);
     static constexpr int CH = kStageBytes / (2 * D * kElt);         // keys of a chunk
+    static constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
+    static_assert(CH == 1 << kChShift, "chunks are whole boxes");
     static constexpr int MB = CH / 16;                              // blocks of 16 keys
-    static constexpr int kUnit = CH * kWarps;
+    static constexpr int kUnit = CH * W;
     static constexpr int kVOff = CH * D * kElt;                     // values behind the keys of a stage
     static constexpr int kBoxCols = INT8 ? 1 : D / 64;              // boxes side by side in a row of 16-bit values
+    static constexpr int kScaleBytes = INT8 ? W * kStages * CH * 8 : 0;
+    static constexpr int kSmemBytes = kRingBytes + kScaleBytes + 1024;
     static constexpr int kFrag = (D / 16) * NB * 32;                // float4 fragments of a row's O
     // The probabilities are carried 2^14 times as large in FP16, so that what the rounding loses is below 2^-28 of the
-    // largest instead of 2^-14.  bfloat16 has FP32's exponents.
+    // largest instead of 2^-14.  bfloat16 has FP32's exponents.  The running maximum is moved only when a score exceeds it by
+    // more than kLine (log2 units): 2^(14 + 1.5) fits FP16, and a chunk whose maximum need not be known costs no shuffles.
     static constexpr bool kHalfP = INT8 || std::is_same<T, __half>::value;
     static constexpr float kOff = kHalfP ? 14.f : 0.f;
     static constexpr float kUnOff = kHalfP ? 6.103515625e-5f : 1.f;
+    static constexpr float kLine = kHalfP ? 1.5f : 8.f;
     static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
 };
+constexpr float kNoMax = -1e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
 
 // ---------------------------------------------------------------------------------------------------- warp-level pieces
 template <bool BF16>
@@ -231,36 +242,120 @@ __device__ __forceinline__ void write_out(const PagedDecodeParams& prm, int b, i
 
 // ---------------------------------------------------------------------------------------------------- the step
 template <class T, int D, bool INT8, int NB>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+__global__ void __launch_bounds__(Cfg<T, D, INT8, NB>::kThreads, kCtasPerSm)
 paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     using C = Cfg<T, D, INT8, NB>;
-    constexpr int CH = C::CH, MB = C::MB;
+    constexpr int CH = C::CH, MB = C::MB, W = C::W, kStageBytes = C::kStageBytes;
     constexpr bool BF16 = !C::kHalfP;
     extern __shared__ uint8_t smem[];
-    __shared__ __align__(8) uint64_t full_bar[kWarps][kStages];
-    __shared__ int page_s[kWarps][kStages][kMaxBoxes];               // pages of the chunk in a stage; -1: a hole
-    __shared__ float m_s[kWarps][8 * NB], z_s[kWarps][8 * NB], v_ref_s[kWarps];
-    __shared__ int held_s[kWarps];
+    __shared__ __align__(8) uint64_t full_bar[W][kStages], empty_bar[W][kStages];
+    __shared__ uint32_t hole_s[W][kStages];                          // bit i: page i of the chunk in the stage is a hole
+    __shared__ float m_s[W][8 * NB], z_s[W][8 * NB], v_ref_s[W];
+    __shared__ int held_s[W];
+    __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     uint8_t* ring = smem + ((1024u - (ptx::smem_u32(smem) & 1023u)) & 1023u);      // (the swizzle's pattern repeats every 1 KB)
     const PagedCache& c = prm.c;
-    const int page_mask = (1 << c.page_shift) - 1;
-    constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
-    const int box_shift = min(c.page_shift, kChShift), box_rows = 1 << box_shift;
 
-    if (lane == 0) {
-        for (int s = 0; s < kStages; ++s) ptx::mbar_init(ptx::smem_u32(&full_bar[warp][s]), 1);
+    if (tid == 0) {
+        for (int i = 0; i < W * kStages; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&full_bar[0][0] + i), 1);
+            ptx::mbar_init(ptx::smem_u32(&empty_bar[0][0] + i), 1);
+        }
+        abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::tma_prefetch_desc(&k_map);
         ptx::tma_prefetch_desc(&v_map);
     }
-    __syncwarp();
+    __syncthreads();
     ptx::griddep_wait();                     // the cache, the lengths and the queries may be the work of the kernel before
     ptx::griddep_launch_dependents();
+
+    // Bounded wait; false when the CTA gives up.
+    auto wait_bar = [&](uint64_t* b, uint32_t parity) -> bool {
+        const uint32_t bar = ptx::smem_u32(b);
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+        const uint64_t begin = ptx::globaltimer_ns();
+        uint32_t spins = 0;
+        while (!ptx::mbar_try_wait(bar, parity)) {
+            if ((++spins & 63u) != 0u) continue;
+            if (*reinterpret_cast<volatile int*>(&abort_flag)) return false;
+            if (ptx::globaltimer_ns() - begin > prm.wait_limit_ns) {
+                *reinterpret_cast<volatile int*>(&abort_flag) = 1;
+                return false;
+            }
+        }
+        return true;
+    };
 
     int total, used;
     const int cta = blockIdx.x;
     Cursor cc = find_run(prm, C::kUnit, cta, gridDim.x, &total, &used);
+
+    if (warp == W) {
+        // ================================================================ copies: lane w feeds the ring of warp w
+        const int page_mask = (1 << c.page_shift) - 1, box_shift = min(c.page_shift, C::kChShift), box_rows = 1 << box_shift;
+        const uint32_t stages = ptx::smem_u32(ring) + lane * (kStages * kStageBytes);
+        const uint32_t scales = ptx::smem_u32(ring) + kRingBytes + lane * (kStages * CH * 8);
+        int issued = 0;
+        bool ok = true;
+#pragma unroll 1
+        while (cc.left > 0) {
+            const int start = (cc.unit * W + lane) * CH;
+            if (lane < W && start < cc.len) {
+                const int s = issued % kStages, boxes = (min(CH, cc.len - start) + box_rows - 1) >> box_shift;
+                const int hk = cc.h / prm.groups;
+                int page[CH / 16];
+                uint32_t holes = 0u;
+#pragma unroll
+                for (int i = 0; i < CH / 16; ++i) {
+                    page[i] = i < boxes ? paged_page(c, cc.b, start + (i << box_shift)) : -1;
+                    if (page[i] < 0) holes |= 1u << i;
+                }
+                if (issued >= kStages) ok = wait_bar(&empty_bar[lane][s], (issued / kStages - 1) & 1);
+                if (ok && issued != prm.drop_chunk) {
+                    const uint32_t bar = ptx::smem_u32(&full_bar[lane][s]);
+                    const int there = boxes - __popc(holes & ((1u << boxes) - 1u));
+                    hole_s[lane][s] = holes;
+                    ptx::mbar_arrive_expect_tx(bar, (boxes << box_shift) * (2 * D * C::kElt) + (INT8 ? (there << box_shift) * 8 : 0));
+#pragma unroll
+                    for (int i = 0; i < CH / 16; ++i) {
+                        if (i >= boxes) break;
+                        const int row = (start + (i << box_shift)) & page_mask;
+                        // (a hole's box lies outside the map: zeros arrive, nothing is read)
+                        const uint32_t dst = stages + s * kStageBytes + (i << box_shift) * (INT8 ? D : 128);
+#pragma unroll
+                        for (int col = 0; col < C::kBoxCols; ++col) {
+                            ptx::tma_load_4d(dst + col * (CH * 128), &k_map, bar, col * 64, row, hk, page[i]);
+                            ptx::tma_load_4d(dst + col * (CH * 128) + C::kVOff, &v_map, bar, col * 64, row, hk, page[i]);
+                        }
+                        if constexpr (INT8) {
+                            if (page[i] >= 0) {
+                                const int64_t at = ((static_cast<int64_t>(page[i]) * c.Hk + hk) << c.page_shift) + row;
+                                const uint32_t sdst = scales + s * (CH * 8) + (i << box_shift) * 4;
+                                ptx::bulk_load_1d(sdst, c.k_scale + at, box_rows * 4, bar);
+                                ptx::bulk_load_1d(sdst + CH * 4, c.v_scale + at, box_rows * 4, bar);
+                            }
+                        }
+                    }
+                }
+                if (ok) ++issued;
+            }
+            if (__any_sync(0xffffffffu, !ok)) break;
+            next_unit(cc, prm, C::kUnit);
+        }
+        // a CTA that has given up: the copies that are still on the way land before the shared memory is given back
+        if (__any_sync(0xffffffffu, !ok) && lane < W) {
+            for (int i = max(0, issued - kStages); i < issued; ++i) {
+                if (i == prm.drop_chunk) continue;
+                for (int spin = 0; spin < (1 << 16); ++spin)
+                    if (ptx::mbar_try_wait(ptx::smem_u32(&full_bar[lane][i % kStages]), (i / kStages) & 1)) break;
+            }
+        }
+        return;
+    }
+
+    // ==================================================================== products
     // What the joining kernel finds for this CTA: the first CTA that begins inside a row joins that row.
     if (tid == 0) {
         int4 job = make_int4(-1, 0, 0, 0);
@@ -279,100 +374,25 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
     // sequences without a key
     for (int b = cta; b < c.B; b += gridDim.x) {
         if (paged_len(c, b) > 0) continue;
-        for (int i = tid; i < prm.Hq * (D / 8); i += kThreads) {
+        for (int i = tid; i < prm.Hq * (D / 8); i += 32 * W) {
             const int hq = i / (D / 8);
             reinterpret_cast<uint4*>(prm.out + b * prm.os[0] + hq * prm.os[1])[i - hq * (D / 8)] = make_uint4(0u, 0u, 0u, 0u);
         }
         if (prm.lse != nullptr)
-            for (int hq = tid; hq < prm.Hq; hq += kThreads) prm.lse[static_cast<int64_t>(b) * prm.Hq + hq] = -INFINITY;
+            for (int hq = tid; hq < prm.Hq; hq += 32 * W) prm.lse[static_cast<int64_t>(b) * prm.Hq + hq] = -INFINITY;
     }
 
+    const int box_shift = min(c.page_shift, C::kChShift);
     const uint32_t ring_u32 = ptx::smem_u32(ring) + warp * (kStages * kStageBytes);
-    Cursor ic = cc;                          // of the copies, ahead of the one of the products
-    int issued = 0, taken = 0;
-    bool failed = false;                     // a wait ran out: no more copies, and the rows from here on are NaN
-    int failed_at = 0;
-
-    // Starts the copies of this warp's next chunk, if there is one, into the stage that is free.
-    auto issue = [&]() {
-        int start = 0;
-        while (ic.left > 0) {
-            start = (ic.unit * kWarps + warp) * CH;
-            if (start < ic.len) break;
-            next_unit(ic, prm, C::kUnit);
-        }
-        if (ic.left <= 0) return;
-        const int s = issued % kStages;
-        {
-            const int boxes = (min(CH, ic.len - start) + box_rows - 1) >> box_shift;
-            const uint32_t bar = ptx::smem_u32(&full_bar[warp][s]);
-            const int hk = ic.h / prm.groups;
-            int page = -1, row = 0;
-            if (lane < boxes) {
-                const int pos = start + lane * box_rows;
-                page = paged_page(c, ic.b, pos);
-                row = pos & page_mask;
-                page_s[warp][s][lane] = page;
-            }
-            const bool drop = issued == prm.drop_chunk;
-            if (lane == 0 && !drop) ptx::mbar_arrive_expect_tx(bar, boxes * box_rows * (2 * D * C::kElt));
-            __syncwarp();
-            if (lane < boxes && !drop) {
-                // (a hole's box lies outside the map: zeros arrive, nothing is read)
-                const uint32_t dst = ring_u32 + s * kStageBytes + lane * box_rows * (INT8 ? D : 128);
-#pragma unroll
-                for (int col = 0; col < C::kBoxCols; ++col) {
-                    ptx::tma_load_4d(dst + col * (CH * 128), &k_map, bar, col * 64, row, hk, page);
-                    ptx::tma_load_4d(dst + col * (CH * 128) + C::kVOff, &v_map, bar, col * 64, row, hk, page);
-                }
-            }
-        }
-        ++issued;
-        next_unit(ic, prm, C::kUnit);
-    };
-    // Bounded wait for chunk number `taken`.
-    auto landed = [&]() -> bool {
-        const uint32_t bar = ptx::smem_u32(&full_bar[warp][taken % kStages]), parity = (taken / kStages) & 1;
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-        const uint64_t begin = ptx::globaltimer_ns();
-        uint32_t spins = 0;
-        while (!ptx::mbar_try_wait(bar, parity))
-            if ((++spins & 63u) == 0u && ptx::globaltimer_ns() - begin > prm.wait_limit_ns) return false;
-        return true;
-    };
-
-#pragma unroll 1
-    for (int s = 0; s < kStages; ++s) issue();
-    __syncwarp();
-
-    bool first_segment = true;
+    const float* scale_ring = reinterpret_cast<const float*>(ring + kRingBytes) + warp * (kStages * CH * 2);
+    int stage = 0;
+    uint32_t phase = 0u;
+    bool failed = false, first_segment = true;
 #pragma unroll 1
     while (cc.left > 0) {
         // ------------------------------------------------ a row, or this CTA's part of it
         const int u_end = min(cc.n_units, cc.unit + cc.left);
         const int hk = cc.h / prm.groups, q_first = (cc.h - hk * prm.groups) * 8 * NB;
-        // scales of the block's keys of rows g and g + 8 of chunk `number`, whose first key is `start`
-        float dk[MB][2], dv[MB][2];
-        auto load_scales = [&](int number, int start, float (&xk)[MB][2], float (&xv)[MB][2]) {
-            if constexpr (INT8) {
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    const int pos = start + 16 * mb;
-                    const int page = pos < cc.len ? page_s[warp][number % kStages][16 * mb >> box_shift] : -1;
-                    const int64_t at = ((static_cast<int64_t>(page) * c.Hk + hk) << c.page_shift) + (pos & page_mask);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int key = 8 * i + key_of_row<D>(g);
-                        const bool on = page >= 0 && pos + key < cc.len;
-                        xk[mb][i] = on ? __ldcg(c.k_scale + at + key) : 0.f;
-                        xv[mb][i] = on ? __ldcg(c.v_scale + at + key) : 0.f;
-                    }
-                }
-            }
-        };
-        int start = (cc.unit * kWarps + warp) * CH;
-        const int end = min(cc.len, u_end * C::kUnit);        // keys of this segment
-        if (start < end && !failed) load_scales(taken, start, dk, dv);
 
         // ---- query fragments: the right operand (columns = heads g of the block), and what a score is multiplied by
         uint32_t qf[NB][D / 16][2];
@@ -381,6 +401,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
         for (int nb = 0; nb < NB; ++nb) {
             const bool on = q_first + 8 * nb + g < prm.R;
             const uint8_t* row = prm.q + cc.b * prm.qs[0] + (static_cast<int64_t>(hk) * prm.R + q_first + 8 * nb + g) * prm.qs[1];
+            q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
             if constexpr (INT8) {
                 // fragment 4 j + w holds features 16 (t + 4 j) + 4 w .. + 3, as the codes come
 #pragma unroll
@@ -392,7 +413,6 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
                         qf[nb][4 * j + 2 * i][0] = x.x; qf[nb][4 * j + 2 * i][1] = x.y;
                         qf[nb][4 * j + 2 * i + 1][0] = x.z; qf[nb][4 * j + 2 * i + 1][1] = x.w;
                     }
-                q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
                 if constexpr (std::is_same<T, __nv_bfloat16>::value) {
                     // bfloat16 queries as FP16: multiplied by the power of two that brings the row's largest value to
                     // [2^13, 2^14); eight mantissa bits fit, and what becomes subnormal is below 2^-27 of the largest
@@ -424,14 +444,13 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
                         qf[nb][i][k] = on ? __ldcg(reinterpret_cast<const uint32_t*>(row + 32 * i + 16 * k) + t) : 0u;
-                q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
             }
         }
 
         float m_run[NB][2], z[NB][2], acc[D / 16][NB][4];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            m_run[nb][0] = m_run[nb][1] = -INFINITY;
+            m_run[nb][0] = m_run[nb][1] = kNoMax;
             z[nb][0] = z[nb][1] = 0.f;
 #pragma unroll
             for (int md = 0; md < D / 16; ++md) acc[md][nb][0] = acc[md][nb][1] = acc[md][nb][2] = acc[md][nb][3] = 0.f;
@@ -439,216 +458,219 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
         // INT8: the scale of a value is folded into its probability relative to v_ref, a power of two at or above every
         // scale so far; O~ is in units of it.
         float v_ref = 7.888609052210118e-31f;                 // 2^-100
+        const int end = min(cc.len, u_end * C::kUnit);        // keys of this segment
         bool any = false;
+        int held = 0;
 
 #pragma unroll 1
-        for (; start < end; start += C::kUnit) {
+        for (int start = (cc.unit * W + warp) * CH; start < end; start += C::kUnit) {
+            if (!failed && !wait_bar(&full_bar[warp][stage], phase)) failed = true;
+            if (failed) break;
             any = true;
-            const bool more = start + C::kUnit < end;
-            float dk_next[MB][2], dv_next[MB][2];
-            if (more && !failed) load_scales(taken + 1, start + C::kUnit, dk_next, dv_next);
-            if (!failed && !landed()) {
-                failed = true;
-                failed_at = taken;
-            }
-            if (!failed) {
-                const int s = taken % kStages;
-                const uint32_t kst = ring_u32 + s * kStageBytes, vst = kst + C::kVOff;
-                const int live = min(CH, cc.len - start);               // keys of the chunk
-                const int blocks = (live + 15) / 16;
-                // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same)
-                float sc[MB][NB][4];
+            const uint32_t kst = ring_u32 + stage * kStageBytes, vst = kst + C::kVOff;
+            const int live = min(CH, cc.len - start);         // keys of the chunk
+            const uint32_t holes = hole_s[warp][stage];
+            const bool partial = live < CH || (holes & ((1u << (CH >> box_shift)) - 1u)) != 0u;
+            // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same)
+            float sc[MB][NB][4], v_mul[MB][2];
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
+            for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) sc[mb][nb][0] = sc[mb][nb][1] = sc[mb][nb][2] = sc[mb][nb][3] = 0.f;
-                    if (mb < blocks) {
-                        if constexpr (INT8) {
-                            const int r0 = 16 * mb + key_of_row<D>(g);
+                for (int nb = 0; nb < NB; ++nb) sc[mb][nb][0] = sc[mb][nb][1] = sc[mb][nb][2] = sc[mb][nb][3] = 0.f;
+                if constexpr (INT8) {
+                    const int r0 = 16 * mb + key_of_row<D>(g);
 #pragma unroll
-                            for (int j = 0; j < D / 64; ++j) {
-                                const uint4 xa = lds128(kst + code_piece<D>(r0, t + 4 * j)), xb = lds128(kst + code_piece<D>(r0 + 8, t + 4 * j));
-                                const uint32_t wa[4] = {xa.x, xa.y, xa.z, xa.w}, wb[4] = {xb.x, xb.y, xb.z, xb.w};
+                    for (int j = 0; j < D / 64; ++j) {
+                        const uint4 xa = lds128(kst + code_piece<D>(r0, t + 4 * j)), xb = lds128(kst + code_piece<D>(r0 + 8, t + 4 * j));
+                        const uint32_t wa[4] = {xa.x, xa.y, xa.z, xa.w}, wb[4] = {xb.x, xb.y, xb.z, xb.w};
 #pragma unroll
-                                for (int w = 0; w < 4; ++w) {
-                                    const uint32_t ua = wa[w] ^ 0x80808080u, ub = wb[w] ^ 0x80808080u;
-                                    const uint32_t a0 = codes_to_half2<false>(ua), a2 = codes_to_half2<true>(ua);
-                                    const uint32_t a1 = codes_to_half2<false>(ub), a3 = codes_to_half2<true>(ub);
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t ua = wa[w] ^ 0x80808080u, ub = wb[w] ^ 0x80808080u;
+                            const uint32_t a0 = codes_to_half2<false>(ua), a2 = codes_to_half2<true>(ua);
+                            const uint32_t a1 = codes_to_half2<false>(ub), a3 = codes_to_half2<true>(ub);
 #pragma unroll
-                                    for (int nb = 0; nb < NB; ++nb)
-                                        mma_16816<false>(sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
-                                }
-                            }
-                        } else {
-                            const int row = 16 * mb + (lane & 15), piece = lane >> 4;
-#pragma unroll
-                            for (int i = 0; i < D / 16; ++i) {
-                                uint32_t a[4];
-                                ldmatrix_x4<false>(a, kst + value_piece<CH>(row, 2 * i + piece));
-#pragma unroll
-                                for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
-                            }
+                            for (int nb = 0; nb < NB; ++nb)
+                                mma_16816<false>(sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
                         }
                     }
+                    const float* sk = scale_ring + stage * (CH * 2) + r0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float dk = sk[8 * i];
+                        v_mul[mb][i] = sk[CH + 8 * i];
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) { sc[mb][nb][2 * i] *= dk; sc[mb][nb][2 * i + 1] *= dk; }
+                    }
+                } else {
+                    const int row = 16 * mb + (lane & 15), piece = lane >> 4;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint32_t a[4];
+                        ldmatrix_x4<false>(a, kst + value_piece<CH>(row, 2 * i + piece));
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
+                    }
                 }
-                // ---- scales; keys past the end and in holes do not exist
-                uint32_t dv_top = 0u;
+            }
+            // ---- keys past the end and in holes do not exist, whatever lies in their rows
+            if (partial) {
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb) {
-                    const bool hole = mb < blocks && page_s[warp][s][16 * mb >> box_shift] < 0;
+                    const bool hole = (holes >> (16 * mb >> box_shift)) & 1u;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int key = 16 * mb + 8 * i + (INT8 ? key_of_row<D>(g) : g);
-                        const bool on = key < live && !hole;
+                        if (key < live && !hole) continue;
 #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                float x = sc[mb][nb][2 * i + k];
-                                if constexpr (INT8) x *= dk[mb][i];
-                                sc[mb][nb][2 * i + k] = on ? x : -INFINITY;
-                            }
-                        if constexpr (INT8) dv_top = max(dv_top, __float_as_uint(dv[mb][i]) & 0x7fffffffu);
+                        for (int nb = 0; nb < NB; ++nb) sc[mb][nb][2 * i] = sc[mb][nb][2 * i + 1] = -INFINITY;
+                        v_mul[mb][i] = 0.f;
                     }
                 }
-                // ---- running maximum, over the lanes of a column; alpha brings what has been summed to the new one
-                float sub[NB][2], alpha[NB][2];
+                if constexpr (!INT8) {
+                    // (0 times a NaN is one)
+                    for (int i = lane; i < (CH - live) * (D / 8); i += 32) {
+                        const int row = live + i / (D / 8), piece = i & (D / 8 - 1);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vst + value_piece<CH>(row, piece)), "r"(0u) : "memory");
+                    }
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                }
+            }
+            // ---- exponents, relative to the running maximum; it moves when one of them passes the line
+            float top = -INFINITY;
+            auto exponents = [&](float (&e)[MB][NB][4]) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], C::kOff - m_run[nb][k & 1]);
+            };
+            float e[MB][NB][4];
+            exponents(e);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) top = fmax3(fmax3(top, e[mb][nb][0], e[mb][nb][1]), e[mb][nb][2], e[mb][nb][3]);
+            bool past = top > C::kOff + C::kLine;
+            if constexpr (INT8) {
+                float v_top = fmaxf(v_mul[0][0], v_mul[0][1]);
+#pragma unroll
+                for (int mb = 1; mb < MB; ++mb) v_top = fmax3(v_top, v_mul[mb][0], v_mul[mb][1]);
+                past = past || v_top > v_ref;
+            }
+            if (__any_sync(0xffffffffu, past)) {
+                float alpha[NB][2];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        float top = fmaxf(sc[0][nb][k], sc[0][nb][2 + k]);
+                        float x = fmaxf(sc[0][nb][k], sc[0][nb][2 + k]);
 #pragma unroll
-                        for (int mb = 1; mb < MB; ++mb) top = fmax3(top, sc[mb][nb][k], sc[mb][nb][2 + k]);
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                        const float m_new = fmaxf(m_run[nb][k], top * q_mul[nb][k]);
-                        const float m_use = m_new == -INFINITY ? 0.f : m_new;      // (nothing but holes so far)
-                        alpha[nb][k] = exp2f(m_run[nb][k] - m_use);
-                        sub[nb][k] = C::kOff - m_use;
+                        for (int mb = 1; mb < MB; ++mb) x = fmax3(x, sc[mb][nb][k], sc[mb][nb][2 + k]);
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                        const float m_new = fmaxf(m_run[nb][k], x * q_mul[nb][k]);
+                        alpha[nb][k] = exp2f(m_run[nb][k] - m_new);
                         m_run[nb][k] = m_new;
                         z[nb][k] *= alpha[nb][k];
                     }
-                float v_mul[MB][2];
                 if constexpr (INT8) {
-                    dv_top = __reduce_max_sync(0xffffffffu, dv_top);
-                    const uint32_t want = (min(dv_top, 0x7e800000u) + 0x7fffffu) & 0x7f800000u, have = __float_as_uint(v_ref);
+                    uint32_t dv = 0u;
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) dv = max(dv, max(__float_as_uint(fabsf(v_mul[mb][0])), __float_as_uint(fabsf(v_mul[mb][1]))));
+                    dv = __reduce_max_sync(0xffffffffu, dv);
+                    const uint32_t want = (min(dv, 0x7e800000u) + 0x7fffffu) & 0x7f800000u, have = __float_as_uint(v_ref);
                     if (want > have) {          // (the same in the whole warp)
                         const float back = __uint_as_float(have) * __uint_as_float(0x7f000000u - want);
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) { alpha[nb][0] *= back; alpha[nb][1] *= back; }
                         v_ref = __uint_as_float(want);
                     }
-                    const float inv = __uint_as_float(0x7f000000u - __float_as_uint(v_ref));
-#pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) { v_mul[mb][0] = dv[mb][0] * inv; v_mul[mb][1] = dv[mb][1] * inv; }
                 }
-                bool still = true;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) still = still && alpha[nb][0] == 1.f && alpha[nb][1] == 1.f;
-                if (!__all_sync(0xffffffffu, still)) {
-#pragma unroll
-                    for (int md = 0; md < D / 16; ++md)
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) {
-                            acc[md][nb][0] *= alpha[nb][0]; acc[md][nb][1] *= alpha[nb][1];
-                            acc[md][nb][2] *= alpha[nb][0]; acc[md][nb][3] *= alpha[nb][1];
-                        }
-                }
-                // ---- probabilities, and O^T += V^T P^T block by block
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    if (mb >= blocks) continue;
-                    uint32_t p0[NB], p1[NB];
+                for (int md = 0; md < D / 16; ++md)
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
-                        float p[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            p[k] = fast_exp2(fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]));
-                            z[nb][k & 1] += p[k];
-                            if constexpr (INT8) p[k] *= v_mul[mb][k >> 1];
-                        }
-                        using P = typename std::conditional<C::kHalfP, __half, __nv_bfloat16>::type;
-                        p0[nb] = transpose_8x8(act_pack2(p[0], p[1], P()));
-                        p1[nb] = transpose_8x8(act_pack2(p[2], p[3], P()));
+                        acc[md][nb][0] *= alpha[nb][0]; acc[md][nb][1] *= alpha[nb][1];
+                        acc[md][nb][2] *= alpha[nb][0]; acc[md][nb][3] *= alpha[nb][1];
                     }
-                    if constexpr (INT8) {
-                        // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
-                        const int r0 = 16 * mb + key_of_row<D>(2 * t), r1 = 16 * mb + key_of_row<D>(2 * t + 1);
-                        uint32_t x[4][D / 32];
+                exponents(e);
+            }
+            const float inv = __uint_as_float(0x7f000000u - __float_as_uint(v_ref));
+            // ---- probabilities, and O^T += V^T P^T block by block
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int row = (i & 1 ? r1 : r0) + (i >> 1) * 8;
-                            if constexpr (D == 128) {
-                                const uint4 v = lds128(vst + code_piece<D>(row, g));
-                                x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
-                            } else {
-                                const uint2 v = lds64(vst + code_piece<D>(row, g >> 1) + 8 * (g & 1));
-                                x[i][0] = v.x; x[i][1] = v.y;
-                            }
+            for (int mb = 0; mb < MB; ++mb) {
+                uint32_t p0[NB], p1[NB];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    float p[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        p[k] = fast_exp2(e[mb][nb][k]);
+                        z[nb][k & 1] += p[k];
+                        if constexpr (INT8) p[k] *= v_mul[mb][k >> 1] * inv;
+                    }
+                    using P = typename std::conditional<C::kHalfP, __half, __nv_bfloat16>::type;
+                    p0[nb] = transpose_8x8(act_pack2(p[0], p[1], P()));
+                    p1[nb] = transpose_8x8(act_pack2(p[2], p[3], P()));
+                }
+                if constexpr (INT8) {
+                    // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
+                    const int r0 = 16 * mb + key_of_row<D>(2 * t), r1 = 16 * mb + key_of_row<D>(2 * t + 1);
+                    uint32_t x[4][D / 32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int row = (i & 1 ? r1 : r0) + (i >> 1) * 8;
+                        if constexpr (D == 128) {
+                            const uint4 v = lds128(vst + code_piece<D>(row, g));
+                            x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+                        } else {
+                            const uint2 v = lds64(vst + code_piece<D>(row, g >> 1) + 8 * (g & 1));
+                            x[i][0] = v.x; x[i][1] = v.y;
                         }
+                    }
 #pragma unroll
-                        for (int w = 0; w < D / 32; ++w) {
-                            const uint32_t u0 = x[0][w] ^ 0x80808080u, u1 = x[1][w] ^ 0x80808080u;
-                            const uint32_t u2 = x[2][w] ^ 0x80808080u, u3 = x[3][w] ^ 0x80808080u;
-                            const uint32_t lo01 = __byte_perm(u0, u1, 0x5140), hi01 = __byte_perm(u0, u1, 0x7362);
-                            const uint32_t lo23 = __byte_perm(u2, u3, 0x5140), hi23 = __byte_perm(u2, u3, 0x7362);
+                    for (int w = 0; w < D / 32; ++w) {
+                        const uint32_t u0 = x[0][w] ^ 0x80808080u, u1 = x[1][w] ^ 0x80808080u;
+                        const uint32_t u2 = x[2][w] ^ 0x80808080u, u3 = x[3][w] ^ 0x80808080u;
+                        const uint32_t lo01 = __byte_perm(u0, u1, 0x5140), hi01 = __byte_perm(u0, u1, 0x7362);
+                        const uint32_t lo23 = __byte_perm(u2, u3, 0x5140), hi23 = __byte_perm(u2, u3, 0x7362);
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint32_t a01 = e ? hi01 : lo01, a23 = e ? hi23 : lo23;
-                                const uint32_t a0 = codes_to_half2<false>(a01), a1 = codes_to_half2<true>(a01);
-                                const uint32_t a2 = codes_to_half2<false>(a23), a3 = codes_to_half2<true>(a23);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t a01 = h ? hi01 : lo01, a23 = h ? hi23 : lo23;
+                            const uint32_t a0 = codes_to_half2<false>(a01), a1 = codes_to_half2<true>(a01);
+                            const uint32_t a2 = codes_to_half2<false>(a23), a3 = codes_to_half2<true>(a23);
 #pragma unroll
-                                for (int nb = 0; nb < NB; ++nb) mma_16816<false>(acc[2 * w + e][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
-                            }
+                            for (int nb = 0; nb < NB; ++nb) mma_16816<false>(acc[2 * w + h][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
                         }
-                    } else {
-                        // (what lies behind the last key may be anything, and 0 times a NaN is one)
-                        const bool cut = 16 * mb + 16 > live;
-                        uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
-                        if (cut) {
-                            const int k0 = 16 * mb + 2 * t;
-                            keep0 = (k0 < live ? 0xffffu : 0u) | (k0 + 1 < live ? 0xffff0000u : 0u);
-                            keep1 = (k0 + 8 < live ? 0xffffu : 0u) | (k0 + 9 < live ? 0xffff0000u : 0u);
-                        }
-                        const int row = 16 * mb + (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1;
+                    }
+                } else {
+                    const int row = 16 * mb + (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1;
 #pragma unroll
-                        for (int md = 0; md < D / 16; ++md) {
-                            uint32_t a[4];
-                            ldmatrix_x4<true>(a, vst + value_piece<CH>(row, 2 * md + piece));
-                            a[0] &= keep0; a[1] &= keep0; a[2] &= keep1; a[3] &= keep1;
+                    for (int md = 0; md < D / 16; ++md) {
+                        uint32_t a[4];
+                        ldmatrix_x4<true>(a, vst + value_piece<CH>(row, 2 * md + piece));
 #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
-                        }
+                        for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
                     }
                 }
             }
-            ++taken;
-            __syncwarp();                    // every lane is done with the stage
-            if (more) {
-                if (!failed) issue();
-                __syncwarp();
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    dk[mb][0] = dk_next[mb][0]; dk[mb][1] = dk_next[mb][1];
-                    dv[mb][0] = dv_next[mb][0]; dv[mb][1] = dv_next[mb][1];
-                }
-            }
+            held = stage;
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            __syncwarp();                    // every lane is done with the stage; the segment's last one is kept for the merge
+            if (start + C::kUnit < end && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&empty_bar[warp][held]));
         }
 
         // ------------------------------------------------ the warps' results of the segment, merged in the stages read last
-        // (a warp's last stage of a segment is refilled after the merge; every warp holds the same places of O^T)
-        if (failed)
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) z[nb][0] = z[nb][1] = NAN;
-        const int held = (taken + kStages - 1) % kStages;           // of chunk taken - 1
+        // (every warp holds the same places of O^T; a warp without a chunk here has no stage to itself: its place is not read)
         float4* mine = reinterpret_cast<float4*>(ring + (warp * kStages + held) * kStageBytes);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
+                if (failed) z[nb][k] = NAN;
                 z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 4);
                 z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 8);
                 z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 16);
@@ -659,66 +681,51 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
                 for (int md = 0; md < D / 16; ++md)
                     mine[(md * NB + nb) * 32 + lane] = make_float4(acc[md][nb][0], acc[md][nb][1], acc[md][nb][2], acc[md][nb][3]);
         }
-        // (a warp without a chunk of the segment has no stage to itself: weight 0, and its place is not read)
         if (lane == 0) {
             v_ref_s[warp] = any && !failed ? (INT8 ? v_ref : 1.f) : -1.f;
             held_s[warp] = held;
         }
-        __syncthreads();
+        ptx::bar_sync_named(1, 32 * W);
         {
             const bool whole = cc.unit == 0 && u_end == cc.n_units;
             const int slot = 2 * cta + (first_segment ? 0 : 1);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                float m[2], zz[2], wgt[kWarps][2];
+#pragma unroll 1
+            for (int i = warp; i < (D / 16) * NB; i += W) {
+                const int md = i / NB, nb = i - md * NB;
+                float m[2], zz[2], wgt[W][2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int n = 8 * nb + 2 * t + k;
-                    m[k] = fmaxf(fmaxf(m_s[0][n], m_s[1][n]), fmaxf(m_s[2][n], m_s[3][n]));
-                    const float use = m[k] == -INFINITY ? 0.f : m[k];
+                    m[k] = m_s[0][n];
+#pragma unroll
+                    for (int w = 1; w < W; ++w) m[k] = fmaxf(m[k], m_s[w][n]);
                     zz[k] = 0.f;
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        const float f = exp2f(m_s[w][n] - use) * C::kUnOff;
+                    for (int w = 0; w < W; ++w) {
+                        const float f = exp2f(m_s[w][n] - m[k]) * C::kUnOff;
                         zz[k] += z_s[w][n] * f;
                         wgt[w][k] = f * v_ref_s[w];
                     }
                 }
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < D / 16 / kWarps; ++i) {
-                    const int md = warp + kWarps * i;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        if (v_ref_s[w] < 0.f) continue;
-                        const float4 x = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes)[(md * NB + nb) * 32 + lane];
-                        o.x += x.x * wgt[w][0]; o.y += x.y * wgt[w][1]; o.z += x.z * wgt[w][0]; o.w += x.w * wgt[w][1];
-                    }
-                    if (whole) write_out<T, D, INT8, NB>(prm, cc.b, cc.h, md, nb, lane, o, m, zz);
-                    else prm.part_o[(static_cast<int64_t>(slot) * (D / 16) + md) * (NB * 32) + nb * 32 + lane] = o;
+                for (int w = 0; w < W; ++w) {
+                    if (v_ref_s[w] < 0.f) continue;
+                    const float4 x = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes)[i * 32 + lane];
+                    o.x += x.x * wgt[w][0]; o.y += x.y * wgt[w][1]; o.z += x.z * wgt[w][0]; o.w += x.w * wgt[w][1];
                 }
-                if (!whole && warp == 0 && g == 0) {
-                    prm.part_mz[slot * (8 * NB) + 8 * nb + 2 * t] = make_float2(m[0], zz[0]);
-                    prm.part_mz[slot * (8 * NB) + 8 * nb + 2 * t + 1] = make_float2(m[1], zz[1]);
-                }
+                if (whole) write_out<T, D, INT8, NB>(prm, cc.b, cc.h, md, nb, lane, o, m, zz);
+                else prm.part_o[static_cast<int64_t>(slot) * C::kFrag + i * 32 + lane] = o;
+                if (!whole && md == 0 && g == 0)
+                    *reinterpret_cast<float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t) = make_float4(m[0], zz[0], m[1], zz[1]);
             }
         }
         ptx::fence_proxy_async_smem();       // the stages go back to the copies
-        __syncthreads();
-        if (any && !failed) issue();
-        __syncwarp();
+        ptx::bar_sync_named(1, 32 * W);
+        if (any && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&empty_bar[warp][held]));
         first_segment = false;
         cc.left -= u_end - cc.unit;
         if (cc.left > 0) next_row(cc, prm, C::kUnit);
-    }
-
-    if (failed) {
-        // the copies that are still on the way land before the shared memory is given back
-        for (int i = failed_at; i < issued; ++i) {
-            if (i == prm.drop_chunk) continue;
-            for (int spin = 0; spin < (1 << 16); ++spin)
-                if (ptx::mbar_try_wait(ptx::smem_u32(&full_bar[warp][i % kStages]), (i / kStages) & 1)) break;
-        }
     }
 }
 
@@ -733,6 +740,7 @@ paged_join_kernel(const PagedDecodeParams prm) {
     __shared__ float2 mz_s[kJoinWarps][NB][32][2];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
+    using C = Cfg<T, D, INT8, NB>;
     const int4 job = __ldcg(prm.join + blockIdx.x);
     if (job.x < 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, md = blockIdx.y, parts = job.w + 1;
@@ -741,16 +749,16 @@ paged_join_kernel(const PagedDecodeParams prm) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         o[nb] = make_float4(0.f, 0.f, 0.f, 0.f);
-        m[nb][0] = m[nb][1] = -INFINITY;
+        m[nb][0] = m[nb][1] = kNoMax;
         z[nb][0] = z[nb][1] = 0.f;
     }
     auto add = [&](int nb, const float4& x, const float2 (&mz)[2]) {
         float back[2], fore[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const float top = fmaxf(m[nb][k], mz[k].x), use = top == -INFINITY ? 0.f : top;
-            back[k] = exp2f(m[nb][k] - use);
-            fore[k] = exp2f(mz[k].x - use);
+            const float top = fmaxf(m[nb][k], mz[k].x);
+            back[k] = exp2f(m[nb][k] - top);
+            fore[k] = exp2f(mz[k].x - top);
             z[nb][k] = z[nb][k] * back[k] + mz[k].y * fore[k];
             m[nb][k] = top;
         }
@@ -767,7 +775,7 @@ paged_join_kernel(const PagedDecodeParams prm) {
             const int64_t slot = i == 0 ? job.z : 2 * (static_cast<int>(blockIdx.x) + i - 1);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                x[j][nb] = __ldcg(prm.part_o + (slot * (D / 16) + md) * (NB * 32) + nb * 32 + lane);
+                x[j][nb] = __ldcg(prm.part_o + slot * C::kFrag + (md * NB + nb) * 32 + lane);
                 const float4 two = __ldcg(reinterpret_cast<const float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t));
                 mz[j][nb][0] = make_float2(two.x, two.y);
                 mz[j][nb][1] = make_float2(two.z, two.w);
@@ -809,8 +817,7 @@ int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* p
     const int R = heads_q / p->heads_kv;
     plan->NB = R > 8 ? 2 : 1;
     plan->groups = static_cast<int>(ceil_div(R, 8 * plan->NB));
-    const int elt = p->cache_type == TILEMIX_CACHE_INT8 ? 1 : 2;
-    plan->unit = kWarps * kStageBytes / (2 * p->head_dim * elt);
+    plan->unit = kRingBytes / kStages / (2 * p->head_dim * (p->cache_type == TILEMIX_CACHE_INT8 ? 1 : 2));    // Cfg::kUnit
     const int64_t rows = static_cast<int64_t>(p->heads_kv) * plan->groups;
     const int64_t units = rows * p->batch * ceil_div(c->capacity, plan->unit);
     if (rows > (1 << 24) || units > (int64_t{1} << 30) || static_cast<int64_t>(p->batch) * heads_q > (int64_t{1} << 30)) return TILEMIX_ERR_SHAPE;
@@ -843,16 +850,17 @@ template <class T, int D, bool INT8, int NB>
 int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) {
     using C = Cfg<T, D, INT8, NB>;
     const PagedCache& c = prm.c;
+    static_assert(C::kUnit == kRingBytes / kStages / (2 * D * C::kElt), "see resolve_decode");
     CUtensorMap km, vm;
     const int page = 1 << c.page_shift, box_rows = page < C::CH ? page : C::CH;
     int rc;
     if ((rc = encode_pool_map(&km, c.k_pool, C::kElt, D, page, c.Hk, c.n_pages, c.ks, box_rows))) return rc;
     if ((rc = encode_pool_map(&vm, c.v_pool, C::kElt, D, page, c.Hk, c.n_pages, c.vs, box_rows))) return rc;
     auto kernel = paged_decode_kernel<T, D, INT8, NB>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return static_cast<int>(e);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(plan.ctas); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = stream;
+    cfg.gridDim = dim3(plan.ctas); cfg.blockDim = dim3(C::kThreads); cfg.dynamicSmemBytes = C::kSmemBytes; cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
