@@ -5,10 +5,10 @@
 // warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
 // at the cost of ~17 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.
 //
-// Layout of the work.  A CTA has four or eight warps at the products and one that starts the copies; two CTAs share an SM.
-// Every warp of the first kind owns a ring of three stages and takes CHUNKS of 16 to 64 keys out of it, which one TMA box a
-// page brings in, swizzled (with the scales, where there are any): 192 KB of an SM's shared memory are on the way, and no warp
-// waits for another but at the end of a row.  Neighbouring chunks, one for each warp, are a UNIT; the units of all
+// Layout of the work.  A warp owns a ring of three stages, starts its own copies and takes CHUNKS of 16 to 64 keys, which one
+// TMA box a page brings in, swizzled; no warp waits for another but at the end of a row.  Four or eight warps are a CTA, two
+// CTAs share an SM: 192 KB are on the way.  (A warp of its own for the copies of all could not start them fast
+// enough: four small ones a chunk, 8 x 32K keys of 128 in INT8 129 us, 101 so.)  Neighbouring chunks, one for each warp, are a UNIT; the units of all
 // (sequence, KV head) rows, one row behind the other, are dealt out to the CTAs in equal runs, so that a batch of unequal
 // lengths keeps every SM busy to the end.  A CTA finds its run from the lengths, which only the device knows.  Rows inside
 // its run it finishes itself; of a row that it shares with its neighbours it leaves a partial result (m, z, O) to the joining
@@ -60,9 +60,9 @@ template <class T, int D, bool INT8, int NB>
 struct Cfg {
     static constexpr int kElt = INT8 ? 1 : 2;
     // Warps at the products.  The INT8 form is bound by issue slots and latencies, not by bytes, unless many warps share them
-    // (8 x 32K keys, d = 128: four a CTA 135 us, eight XX us); sixteen query heads need the registers of four.
+    // (8 x 32K keys, d = 128: four a CTA 135 us, eight 101); sixteen query heads need the registers of four.
     static constexpr int W = INT8 && NB == 1 ? 8 : 4;
-    static constexpr int kThreads = 32 * (W + 1);
+    static constexpr int kThreads = 32 * W;
     static constexpr int kStageBytes = kRingBytes / (W * kStages);
     static constexpr int CH = kStageBytes / (2 * D * kElt);         // keys of a chunk
     static constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
@@ -248,112 +248,102 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
     constexpr int CH = C::CH, MB = C::MB, W = C::W, kStageBytes = C::kStageBytes;
     constexpr bool BF16 = !C::kHalfP;
     extern __shared__ uint8_t smem[];
-    __shared__ __align__(8) uint64_t full_bar[W][kStages], empty_bar[W][kStages];
-    __shared__ uint32_t hole_s[W][kStages];                          // bit i: page i of the chunk in the stage is a hole
+    __shared__ __align__(8) uint64_t full_bar[W][kStages];
+    __shared__ uint32_t hole_s[W][kStages];                          // bit 4 i: the 16 keys i of the chunk lie in a hole
     __shared__ float m_s[W][8 * NB], z_s[W][8 * NB], v_ref_s[W];
     __shared__ int held_s[W];
-    __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     uint8_t* ring = smem + ((1024u - (ptx::smem_u32(smem) & 1023u)) & 1023u);      // (the swizzle's pattern repeats every 1 KB)
     const PagedCache& c = prm.c;
 
-    if (tid == 0) {
-        for (int i = 0; i < W * kStages; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&full_bar[0][0] + i), 1);
-            ptx::mbar_init(ptx::smem_u32(&empty_bar[0][0] + i), 1);
-        }
-        abort_flag = 0;
+    if (lane == 0) {
+        // (arrivals: the lane that announces the bytes of the boxes, and every lane with its part of the scales)
+        for (int i = 0; i < kStages; ++i) ptx::mbar_init(ptx::smem_u32(&full_bar[warp][i]), INT8 ? 33 : 1);
         ptx::fence_mbar_init();
         ptx::tma_prefetch_desc(&k_map);
         ptx::tma_prefetch_desc(&v_map);
     }
-    __syncthreads();
+    __syncwarp();
     ptx::griddep_wait();                     // the cache, the lengths and the queries may be the work of the kernel before
     ptx::griddep_launch_dependents();
-
-    // Bounded wait; false when the CTA gives up.
-    auto wait_bar = [&](uint64_t* b, uint32_t parity) -> bool {
-        const uint32_t bar = ptx::smem_u32(b);
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-        const uint64_t begin = ptx::globaltimer_ns();
-        uint32_t spins = 0;
-        while (!ptx::mbar_try_wait(bar, parity)) {
-            if ((++spins & 63u) != 0u) continue;
-            if (*reinterpret_cast<volatile int*>(&abort_flag)) return false;
-            if (ptx::globaltimer_ns() - begin > prm.wait_limit_ns) {
-                *reinterpret_cast<volatile int*>(&abort_flag) = 1;
-                return false;
-            }
-        }
-        return true;
-    };
 
     int total, used;
     const int cta = blockIdx.x;
     Cursor cc = find_run(prm, C::kUnit, cta, gridDim.x, &total, &used);
 
-    if (warp == W) {
-        // ================================================================ copies: lane w feeds the ring of warp w
-        const int page_mask = (1 << c.page_shift) - 1, box_shift = min(c.page_shift, C::kChShift), box_rows = 1 << box_shift;
-        const uint32_t stages = ptx::smem_u32(ring) + lane * (kStages * kStageBytes);
-        const uint32_t scales = ptx::smem_u32(ring) + kRingBytes + lane * (kStages * CH * 8);
-        int issued = 0;
-        bool ok = true;
+    // ---- copies.  `prepare` finds this warp's next chunk and looks its pages up, every lane that of four of its keys;
+    // `fire` starts its copies into the stage behind the one filled last.
+    const int box_shift = min(c.page_shift, C::kChShift), page_mask = (1 << c.page_shift) - 1;
+    const uint32_t ring_u32 = ptx::smem_u32(ring) + warp * (kStages * kStageBytes);
+    const uint32_t scale_u32 = ptx::smem_u32(ring) + kRingBytes + warp * (kStages * CH * 8);
+    constexpr int kQuads = CH / 4;
+    const int quad = 4 * (lane & (kQuads - 1));
+    Cursor ic = cc;
+    int issued = 0, fill = 0, next_start = 0, next_len = 0, next_hk = 0, next_page = -1;
+    bool next_there = false;
+    auto prepare = [&]() {
+        next_there = false;
+        while (ic.left > 0) {
+            next_start = (ic.unit * W + warp) * CH;
+            if (next_start < ic.len) {
+                next_there = true;
+                break;
+            }
+            next_unit(ic, prm, C::kUnit);
+        }
+        if (!next_there) return;
+        next_len = ic.len;
+        next_hk = prm.groups == 1 ? ic.h : ic.h / prm.groups;
+        next_page = next_start + quad < next_len ? paged_page(c, ic.b, next_start + quad) : -1;
+        next_unit(ic, prm, C::kUnit);
+    };
+    auto fire = [&]() {
+        if (!next_there) return;
+        const uint32_t bar = ptx::smem_u32(&full_bar[warp][fill]);
+        const uint32_t holes = __ballot_sync(0xffffffffu, next_page < 0 && next_start + quad < next_len);
+        if (lane == 0) hole_s[warp][fill] = holes;
+        if (issued != prm.drop_chunk) {
+            const int boxes = (min(CH, next_len - next_start) + (1 << box_shift) - 1) >> box_shift, row = next_start & page_mask;
+            if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (boxes << box_shift) * (2 * D * C::kElt));
+            const uint32_t dst = ring_u32 + fill * kStageBytes;
+#pragma unroll
+            for (int i = 0; i < CH / 16; ++i) {
+                if (i >= boxes) break;
+                // (a hole's box lies outside the map: zeros arrive, nothing is read; more boxes than one: whole pages)
+                const int page = __shfl_sync(0xffffffffu, next_page, i << (box_shift - 2));
+                const uint32_t to = dst + (i << box_shift) * (INT8 ? D : 128);
+#pragma unroll
+                for (int col = 0; col < C::kBoxCols; ++col) {
+                    ptx::tma_load_4d_elect(to + col * (CH * 128), &k_map, bar, col * 64, i == 0 ? row : 0, next_hk, page);
+                    ptx::tma_load_4d_elect(to + col * (CH * 128) + C::kVOff, &v_map, bar, col * 64, i == 0 ? row : 0, next_hk, page);
+                }
+            }
+            if constexpr (INT8) {
+                if (lane < 2 * kQuads) {
+                    const float* from = lane < kQuads ? c.k_scale : c.v_scale;
+                    const int64_t at = ((static_cast<int64_t>(next_page) * c.Hk + next_hk) << c.page_shift) + ((next_start + quad) & page_mask);
+                    ptx::cp_async_16(scale_u32 + fill * (CH * 8) + lane * 16, from + (next_page >= 0 ? at : 0), next_page >= 0);
+                }
+                ptx::cp_async_arrive(bar);
+            }
+        }
+        ++issued;
+        if (++fill == kStages) fill = 0;
+        prepare();
+    };
+    // Bounded wait for the chunk in `stage`.
+    auto landed = [&](int stage, uint32_t phase) -> bool {
+        const uint32_t bar = ptx::smem_u32(&full_bar[warp][stage]);
+        if (ptx::mbar_try_wait(bar, phase)) return true;
+        const uint64_t begin = ptx::globaltimer_ns();
+        uint32_t spins = 0;
+        while (!ptx::mbar_try_wait(bar, phase))
+            if ((++spins & 63u) == 0u && ptx::globaltimer_ns() - begin > prm.wait_limit_ns) return false;
+        return true;
+    };
+    prepare();
 #pragma unroll 1
-        while (cc.left > 0) {
-            const int start = (cc.unit * W + lane) * CH;
-            if (lane < W && start < cc.len) {
-                const int s = issued % kStages, boxes = (min(CH, cc.len - start) + box_rows - 1) >> box_shift;
-                const int hk = cc.h / prm.groups;
-                int page[CH / 16];
-                uint32_t holes = 0u;
-#pragma unroll
-                for (int i = 0; i < CH / 16; ++i) {
-                    page[i] = i < boxes ? paged_page(c, cc.b, start + (i << box_shift)) : -1;
-                    if (page[i] < 0) holes |= 1u << i;
-                }
-                if (issued >= kStages) ok = wait_bar(&empty_bar[lane][s], (issued / kStages - 1) & 1);
-                if (ok && issued != prm.drop_chunk) {
-                    const uint32_t bar = ptx::smem_u32(&full_bar[lane][s]);
-                    const int there = boxes - __popc(holes & ((1u << boxes) - 1u));
-                    hole_s[lane][s] = holes;
-                    ptx::mbar_arrive_expect_tx(bar, (boxes << box_shift) * (2 * D * C::kElt) + (INT8 ? (there << box_shift) * 8 : 0));
-#pragma unroll
-                    for (int i = 0; i < CH / 16; ++i) {
-                        if (i >= boxes) break;
-                        const int row = (start + (i << box_shift)) & page_mask;
-                        // (a hole's box lies outside the map: zeros arrive, nothing is read)
-                        const uint32_t dst = stages + s * kStageBytes + (i << box_shift) * (INT8 ? D : 128);
-#pragma unroll
-                        for (int col = 0; col < C::kBoxCols; ++col) {
-                            ptx::tma_load_4d(dst + col * (CH * 128), &k_map, bar, col * 64, row, hk, page[i]);
-                            ptx::tma_load_4d(dst + col * (CH * 128) + C::kVOff, &v_map, bar, col * 64, row, hk, page[i]);
-                        }
-                        if constexpr (INT8) {
-                            if (page[i] >= 0) {
-                                const int64_t at = ((static_cast<int64_t>(page[i]) * c.Hk + hk) << c.page_shift) + row;
-                                const uint32_t sdst = scales + s * (CH * 8) + (i << box_shift) * 4;
-                                ptx::bulk_load_1d(sdst, c.k_scale + at, box_rows * 4, bar);
-                                ptx::bulk_load_1d(sdst + CH * 4, c.v_scale + at, box_rows * 4, bar);
-                            }
-                        }
-                    }
-                }
-                if (ok) ++issued;
-            }
-            if (__any_sync(0xffffffffu, !ok)) break;
-            next_unit(cc, prm, C::kUnit);
-        }
-        // a CTA that has given up: the copies that are still on the way land before the shared memory is given back
-        if (__any_sync(0xffffffffu, !ok) && lane < W) {
-            for (int i = max(0, issued - kStages); i < issued; ++i) {
-                if (i == prm.drop_chunk) continue;
-                for (int spin = 0; spin < (1 << 16); ++spin)
-                    if (ptx::mbar_try_wait(ptx::smem_u32(&full_bar[lane][i % kStages]), (i / kStages) & 1)) break;
-            }
-        }
-        return;
-    }
+    for (int i = 0; i < kStages; ++i) fire();
 
     // ==================================================================== products
     // What the joining kernel finds for this CTA: the first CTA that begins inside a row joins that row.
@@ -382,12 +372,10 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             for (int hq = tid; hq < prm.Hq; hq += 32 * W) prm.lse[static_cast<int64_t>(b) * prm.Hq + hq] = -INFINITY;
     }
 
-    const int box_shift = min(c.page_shift, C::kChShift);
-    const uint32_t ring_u32 = ptx::smem_u32(ring) + warp * (kStages * kStageBytes);
     const float* scale_ring = reinterpret_cast<const float*>(ring + kRingBytes) + warp * (kStages * CH * 2);
-    int stage = 0;
+    int stage = 0, taken = 0;
     uint32_t phase = 0u;
-    bool failed = false, first_segment = true;
+    bool failed = false, first_segment = true;      // failed: a wait ran out; no more copies, the rows from here on are NaN
 #pragma unroll 1
     while (cc.left > 0) {
         // ------------------------------------------------ a row, or this CTA's part of it
@@ -464,13 +452,13 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
 
 #pragma unroll 1
         for (int start = (cc.unit * W + warp) * CH; start < end; start += C::kUnit) {
-            if (!failed && !wait_bar(&full_bar[warp][stage], phase)) failed = true;
+            if (!failed && !landed(stage, phase)) failed = true;
             if (failed) break;
             any = true;
             const uint32_t kst = ring_u32 + stage * kStageBytes, vst = kst + C::kVOff;
             const int live = min(CH, cc.len - start);         // keys of the chunk
             const uint32_t holes = hole_s[warp][stage];
-            const bool partial = live < CH || (holes & ((1u << (CH >> box_shift)) - 1u)) != 0u;
+            const bool partial = live < CH || holes != 0u;
             // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same)
             float sc[MB][NB][4], v_mul[MB][2];
 #pragma unroll
@@ -516,7 +504,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             if (partial) {
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb) {
-                    const bool hole = (holes >> (16 * mb >> box_shift)) & 1u;
+                    const bool hole = (holes >> (4 * mb)) & 1u;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int key = 16 * mb + 8 * i + (INT8 ? key_of_row<D>(g) : g);
@@ -659,8 +647,9 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             }
             held = stage;
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            ++taken;
             __syncwarp();                    // every lane is done with the stage; the segment's last one is kept for the merge
-            if (start + C::kUnit < end && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&empty_bar[warp][held]));
+            if (start + C::kUnit < end) fire();
         }
 
         // ------------------------------------------------ the warps' results of the segment, merged in the stages read last
@@ -685,7 +674,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             v_ref_s[warp] = any && !failed ? (INT8 ? v_ref : 1.f) : -1.f;
             held_s[warp] = held;
         }
-        ptx::bar_sync_named(1, 32 * W);
+        __syncthreads();
         {
             const bool whole = cc.unit == 0 && u_end == cc.n_units;
             const int slot = 2 * cta + (first_segment ? 0 : 1);
@@ -721,11 +710,20 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             }
         }
         ptx::fence_proxy_async_smem();       // the stages go back to the copies
-        ptx::bar_sync_named(1, 32 * W);
-        if (any && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&empty_bar[warp][held]));
+        __syncthreads();
+        if (any && !failed) fire();
         first_segment = false;
         cc.left -= u_end - cc.unit;
         if (cc.left > 0) next_row(cc, prm, C::kUnit);
+    }
+    if (failed) {
+        // the copies that are still on the way land before the shared memory is given back
+        for (int i = taken; i < issued; ++i) {
+            if (i == prm.drop_chunk) continue;
+            for (int spin = 0; spin < (1 << 16); ++spin)
+                if (ptx::mbar_try_wait(ptx::smem_u32(&full_bar[warp][i % kStages]), (i / kStages) & 1)) break;
+        }
+        ptx::cp_async_wait_all();
     }
 }
 

@@ -82,6 +82,16 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
         : "memory");
 }
 
+// The same by a whole, converged warp with warp-uniform arguments; one elected lane issues the copy.
+__device__ __forceinline__ void tma_load_4d_elect(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5, %6}], [%2];\n\t}"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
+
 // Untiled bulk copy global -> shared memory (one destination CTA): both addresses 16-byte aligned, `bytes` a
 // multiple of 16; completion is counted in bytes on the mbarrier.
 __device__ __forceinline__ void bulk_load_1d(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -90,6 +100,16 @@ __device__ __forceinline__ void bulk_load_1d(uint32_t dst, const void* src, uint
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
         : "memory");
 }
+
+// 16 bytes global -> shared memory by this thread, zeros where `on` is false; cp_async_arrive makes the thread arrive on the
+// mbarrier (one of the arrivals that it was initialised with) when all of its copies so far have landed.
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // ---------------------------------------------------------------- register reallocation
 // Executed by every warp of a warpgroup (4 consecutive warps): hands registers back / takes more.
