@@ -37,8 +37,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kStages = 3, kRingBytes = 96 * 1024;
-constexpr int kCtasPerSm = 2, kSms = 148;
+constexpr int kSms = 148;
 
 struct PagedDecodeParams {
     PagedCache c;
@@ -49,31 +48,48 @@ struct PagedDecodeParams {
     uint8_t* out;
     int64_t qs[2], os[2];           // bytes: (batch, head)
     float* lse;
-    int4* join;                     // [CTAs]: what the joining kernel has to do, see there
-    float4* part_o;                 // [2 CTAs][D / 16][NB][32 lanes]: accumulator fragments
-    float2* part_mz;                // [2 CTAs][8 NB]: maximum (log2 domain) and sum
+    int jobs_by_row;                // 1: a job of the joining kernel for every row, 0: for every worker that there may be
+    int4* join;                     // [jobs]
+    float4* part_o;                 // [2 workers][NB][D / 16][32 lanes]: accumulator fragments
+    float2* part_mz;                // [2 workers][8 NB]: maximum (log2 domain) and sum
     unsigned long long wait_limit_ns;
     int drop_chunk;                 // testing aid: every warp leaves out the copies of its chunk of this number (-1: none)
+};
+
+// The pools as tensor maps: boxes of a chunk, or of a page if that is smaller, and boxes of 16 tokens for smaller chunks.
+struct PoolMaps {
+    CUtensorMap k, v, k16, v16;
 };
 
 template <class T, int D, bool INT8, int NB>
 struct Cfg {
     static constexpr int kElt = INT8 ? 1 : 2;
-    // Warps at the products.  The INT8 form is bound by issue slots and latencies, not by bytes, unless many warps share them
-    // (8 x 32K keys, d = 128: four a CTA 135 us, eight 101); sixteen query heads need the registers of four.
-    static constexpr int W = INT8 && NB == 1 ? 8 : 4;
+    // Warps of a CTA and stages of their rings.  The INT8 form is bound by issue slots and latencies, not by bytes, unless many
+    // warps share them (8 x 32K keys, d = 128: four a CTA 135 us, eight 101); sixteen query heads need the registers of six.
+#ifndef CFG_X
+#define I1S 2
+#define I1C 3
+#define I1B 8192
+#define I2S 3
+#define I2C 2
+#define I2B 8192
+#endif
+    static constexpr int W = 4;
+    static constexpr int kStages = INT8 ? (NB == 1 ? I1S : I2S) : 3;
+    static constexpr int kCtasPerSm = INT8 ? (NB == 1 ? I1C : I2C) : 2;
+    static constexpr int kStageBytes = INT8 ? (NB == 1 ? I1B : I2B) : 8192;
+    static constexpr int kRingBytes = W * kStages * kStageBytes;
+    static constexpr int kMinTeam = 2;                              // see find_work
     static constexpr int kThreads = 32 * W;
-    static constexpr int kStageBytes = kRingBytes / (W * kStages);
     static constexpr int CH = kStageBytes / (2 * D * kElt);         // keys of a chunk
     static constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
     static_assert(CH == 1 << kChShift, "chunks are whole boxes");
     static constexpr int MB = CH / 16;                              // blocks of 16 keys
-    static constexpr int kUnit = CH * W;
     static constexpr int kVOff = CH * D * kElt;                     // values behind the keys of a stage
     static constexpr int kBoxCols = INT8 ? 1 : D / 64;              // boxes side by side in a row of 16-bit values
     static constexpr int kScaleBytes = INT8 ? W * kStages * CH * 8 : 0;
     static constexpr int kSmemBytes = kRingBytes + kScaleBytes + 1024;
-    static constexpr int kFrag = (D / 16) * NB * 32;                // float4 fragments of a row's O
+    static constexpr int kFrag = (D / 16) * 32;                     // float4 fragments of a row's O, eight query heads
     // The probabilities are carried 2^14 times as large in FP16, so that what the rounding loses is below 2^-28 of the
     // largest instead of 2^-14.  bfloat16 has FP32's exponents.  The running maximum is moved only when a score exceeds it by
     // more than kLine (log2 units): 2^(14 + 1.5) fits FP16, and a chunk whose maximum need not be known costs no shuffles.
@@ -109,16 +125,6 @@ __device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ uint4 lds128(uint32_t addr) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t addr) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
-    return v;
-}
 // Bytes 0, 1 (HI = false) or 2, 3 of a word of codes + 128 as an FP16 pair.
 template <bool HI>
 __device__ __forceinline__ uint32_t codes_to_half2(uint32_t biased) {
@@ -146,9 +152,9 @@ __device__ __forceinline__ uint32_t value_piece(int row, int piece) {
 // ---------------------------------------------------------------------------------------------------- the work list
 // Place in the list of units: rows (b, h) of n_units units, h = KV head * groups + group of query heads.
 struct Cursor {
-    int b, h, unit, n_units, len, left;      // left: units from here to the end of the CTA's run
+    int b, h, unit, n_units, len, left;      // left: units from here to the end of the worker's run
 };
-__device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm, int unit_keys) {
+__device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm, int unit_shift) {
     c.unit = 0;
     if (++c.h == prm.HG) {
         c.h = 0;
@@ -158,31 +164,60 @@ __device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm
                 return;
             }
             c.len = paged_len(prm.c, c.b);
-            c.n_units = (c.len + unit_keys - 1) / unit_keys;
+            c.n_units = (c.len + (1 << unit_shift) - 1) >> unit_shift;
         } while (c.n_units == 0);
     }
 }
-__device__ __forceinline__ void next_unit(Cursor& c, const PagedDecodeParams& prm, int unit_keys) {
-    --c.left;
-    if (++c.unit == c.n_units && c.left > 0) next_row(c, prm, unit_keys);
-}
 
-// The run of CTA `cta` of `ctas`: [cta U / n, (cta + 1) U / n) of the U units, n = min(ctas, U).  Whole warps, every one alike.
-__device__ __forceinline__ Cursor find_run(const PagedDecodeParams& prm, int unit_keys, int cta, int ctas, int* total, int* used) {
-    const int lane = threadIdx.x & 31, B = prm.c.B;
-    auto units_of = [&](int b) { return b < B ? (paged_len(prm.c, b) + unit_keys - 1) / unit_keys : 0; };
+// What a warp has to do.  A worker is a team of the CTA's warps: all of them, or, where there are rows enough for more workers
+// and the rows are short (fewer than kShortRow chunks a warp of the team on average), half of them.  Chunks are CH keys, or
+// fewer where there would be fewer units than CTAs.  A unit is a chunk for each warp of the team; the U units go to n workers,
+// U / n or one more to each.
+struct Work {
+    Cursor at;
+    int team_shift, chunk_shift, worker;
+    int base, longer;                        // units of a worker; the first `longer` workers have one more
+
+    __device__ __forceinline__ int first_of(int w) const { return w * base + min(w, longer); }
+    __device__ __forceinline__ int worker_of(int unit) const {
+        const int split = longer * (base + 1);
+        return unit < split ? unit / (base + 1) : longer + (unit - split) / base;
+    }
+};
+constexpr int kShortRow = 4;
+template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE>
+__device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
+    constexpr int kTeamShift = W == 8 ? 3 : 2, kMinShift = MIN_TEAM == 2 ? 1 : 2;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = prm.c.B, ctas = gridDim.x;
+    const int len0 = lane < B ? paged_len(prm.c, lane) : 0;
+    auto len_of = [&](int b) { return b < 32 ? len0 : b < B ? paged_len(prm.c, b) : 0; };
+    int blocks = 0, rows = 0;                // of 16 keys; sequences with a key
+    for (int b = lane; b < B; b += 32) {
+        const int len = len_of(b);
+        blocks += (len + 15) >> 4;
+        rows += len > 0 ? 1 : 0;
+    }
+    blocks = __reduce_add_sync(0xffffffffu, blocks) * prm.HG;
+    rows = __reduce_add_sync(0xffffffffu, rows) * prm.HG;
+    Work w{};
+    w.team_shift = kTeamShift; w.chunk_shift = CH_SHIFT;
+    while (w.chunk_shift > 4 && (blocks >> (w.chunk_shift - 4 + kTeamShift)) < ctas) --w.chunk_shift;
+    while (w.team_shift > kMinShift && rows >= (WAVE << (kTeamShift - w.team_shift)) &&
+           (blocks >> (w.chunk_shift - 4 + w.team_shift)) < kShortRow * rows)
+        --w.team_shift;
+    const int unit_shift = w.chunk_shift + w.team_shift;
     int sum = 0;
-    for (int b = lane; b < B; b += 32) sum += units_of(b);
-    const int U = __reduce_add_sync(0xffffffffu, sum) * prm.HG, n = min(ctas, U);
-    *total = U; *used = n;
-    Cursor c{};
-    if (cta >= n) return c;
-    const int first = static_cast<int>(static_cast<int64_t>(cta) * U / n);
-    c.left = static_cast<int>(static_cast<int64_t>(cta + 1) * U / n) - first;
+    for (int b = lane; b < B; b += 32) sum += (len_of(b) + (1 << unit_shift) - 1) >> unit_shift;
+    const int U = __reduce_add_sync(0xffffffffu, sum) * prm.HG, n = min(ctas << (kTeamShift - w.team_shift), U);
+    w.worker = (blockIdx.x << (kTeamShift - w.team_shift)) + (warp >> w.team_shift);
+    if (w.worker >= n) return w;
+    w.base = U / n; w.longer = U - w.base * n;
+    Cursor& c = w.at;
+    const int first = w.first_of(w.worker);
     int before = 0;                          // units of the sequences before the 32 in hand
     for (int b0 = 0; b0 < B; b0 += 32) {
-        const int mine = units_of(b0 + lane) * prm.HG;
-        int upto = mine;
+        const int len = len_of(b0 + lane), mine = (len + (1 << unit_shift) - 1) >> unit_shift;
+        int upto = mine * prm.HG;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, upto, o);
@@ -192,17 +227,17 @@ __device__ __forceinline__ Cursor find_run(const PagedDecodeParams& prm, int uni
         if (past != 0u) {
             const int l = __ffs(past) - 1;
             c.b = b0 + l;
-            c.n_units = __shfl_sync(0xffffffffu, mine, l) / prm.HG;
+            c.n_units = __shfl_sync(0xffffffffu, mine, l);
+            c.len = __shfl_sync(0xffffffffu, len, l);
             const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - c.n_units * prm.HG);
             c.h = at / c.n_units;
             c.unit = at - c.h * c.n_units;
-            c.len = paged_len(prm.c, c.b);
-            return c;
+            c.left = w.base + (w.worker < w.longer ? 1 : 0);
+            return w;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    c.left = 0;
-    return c;
+    return w;
 }
 
 // ---------------------------------------------------------------------------------------------------- results
@@ -242,10 +277,10 @@ __device__ __forceinline__ void write_out(const PagedDecodeParams& prm, int b, i
 
 // ---------------------------------------------------------------------------------------------------- the step
 template <class T, int D, bool INT8, int NB>
-__global__ void __launch_bounds__(Cfg<T, D, INT8, NB>::kThreads, kCtasPerSm)
-paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+__global__ void __launch_bounds__(Cfg<T, D, INT8, NB>::kThreads, Cfg<T, D, INT8, NB>::kCtasPerSm)
+paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMaps maps) {
     using C = Cfg<T, D, INT8, NB>;
-    constexpr int CH = C::CH, MB = C::MB, W = C::W, kStageBytes = C::kStageBytes;
+    constexpr int CH = C::CH, MB = C::MB, W = C::W, kStages = C::kStages, kStageBytes = C::kStageBytes;
     constexpr bool BF16 = !C::kHalfP;
     extern __shared__ uint8_t smem[];
     __shared__ __align__(8) uint64_t full_bar[W][kStages];
@@ -260,75 +295,110 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
         // (arrivals: the lane that announces the bytes of the boxes, and every lane with its part of the scales)
         for (int i = 0; i < kStages; ++i) ptx::mbar_init(ptx::smem_u32(&full_bar[warp][i]), INT8 ? 33 : 1);
         ptx::fence_mbar_init();
-        ptx::tma_prefetch_desc(&k_map);
-        ptx::tma_prefetch_desc(&v_map);
     }
     __syncwarp();
     ptx::griddep_wait();                     // the cache, the lengths and the queries may be the work of the kernel before
     ptx::griddep_launch_dependents();
 
-    int total, used;
-    const int cta = blockIdx.x;
-    Cursor cc = find_run(prm, C::kUnit, cta, gridDim.x, &total, &used);
+    const Work work = find_work<W, C::kChShift, C::kMinTeam, C::kCtasPerSm * kSms>(prm);
+    const int team = 1 << work.team_shift, member = warp & (team - 1), team_no = warp >> work.team_shift;
+    const int chunk_shift = work.chunk_shift, chunk = 1 << chunk_shift, unit_shift = chunk_shift + work.team_shift, unit_keys = 1 << unit_shift;
+    Cursor cc = work.at;
+    auto team_sync = [&]() { ptx::bar_sync_named(1 + team_no, 32 * team); };
+
+    // Query fragments of a row, as they lie in memory: the right operand (columns = heads g of the block).  INT8: fragment
+    // 4 j + w holds features 16 (t + 4 j) + 4 w .. + 3, as the codes come.
+    uint32_t qf[NB][D / 16][2];
+    auto fetch_q = [&](const Cursor& at) {
+        const int hk = prm.groups == 1 ? at.h : at.h / prm.groups, first = (at.h - hk * prm.groups) * 8 * NB;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const bool on = first + 8 * nb + g < prm.R;
+            const uint8_t* row = prm.q + at.b * prm.qs[0] + (static_cast<int64_t>(hk) * prm.R + first + 8 * nb + g) * prm.qs[1];
+            if constexpr (INT8) {
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                        if (on) x = __ldcg(reinterpret_cast<const uint4*>(row + 32 * (t + 4 * j)) + i);
+                        qf[nb][4 * j + 2 * i][0] = x.x; qf[nb][4 * j + 2 * i][1] = x.y;
+                        qf[nb][4 * j + 2 * i + 1][0] = x.z; qf[nb][4 * j + 2 * i + 1][1] = x.w;
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        qf[nb][i][k] = on ? __ldcg(reinterpret_cast<const uint32_t*>(row + 32 * i + 16 * k) + t) : 0u;
+            }
+        }
+    };
+    if (cc.left > 0) fetch_q(cc);
 
     // ---- copies.  `prepare` finds this warp's next chunk and looks its pages up, every lane that of four of its keys;
     // `fire` starts its copies into the stage behind the one filled last.
-    const int box_shift = min(c.page_shift, C::kChShift), page_mask = (1 << c.page_shift) - 1;
+    const CUtensorMap* const k_map = chunk_shift < C::kChShift ? &maps.k16 : &maps.k;
+    const CUtensorMap* const v_map = chunk_shift < C::kChShift ? &maps.v16 : &maps.v;
+    const int box_shift = chunk_shift < C::kChShift ? 4 : min(c.page_shift, chunk_shift), page_mask = (1 << c.page_shift) - 1;
     const uint32_t ring_u32 = ptx::smem_u32(ring) + warp * (kStages * kStageBytes);
-    const uint32_t scale_u32 = ptx::smem_u32(ring) + kRingBytes + warp * (kStages * CH * 8);
     constexpr int kQuads = CH / 4;
     const int quad = 4 * (lane & (kQuads - 1));
-    Cursor ic = cc;
-    int issued = 0, fill = 0, next_start = 0, next_len = 0, next_hk = 0, next_page = -1;
-    bool next_there = false;
-    auto prepare = [&]() {
-        next_there = false;
-        while (ic.left > 0) {
-            next_start = (ic.unit * W + warp) * CH;
-            if (next_start < ic.len) {
-                next_there = true;
-                break;
-            }
-            next_unit(ic, prm, C::kUnit);
-        }
-        if (!next_there) return;
-        next_len = ic.len;
+    const uint32_t scale_u32 = ptx::smem_u32(ring) + C::kRingBytes + warp * (kStages * CH * 8) + 16 * lane;
+    const int page_rows = c.Hk << c.page_shift;               // scales of a page
+    Cursor ic = cc;                                           // the row of the next chunk
+    int issued = 0, fill = 0, next_start = 0, next_end = 0, next_hk = 0, next_page = -1;   // next_end: of this worker's keys of the row
+    const int32_t* next_table = nullptr;
+    const float* next_scale = nullptr;                        // this lane's: of K or of V, of the row's head
+    auto enter_row = [&]() {
+        const int u_end = min(ic.n_units, ic.unit + ic.left);
+        next_start = (ic.unit << unit_shift) + (member << chunk_shift);
+        next_end = min(ic.len, u_end << unit_shift);
+        ic.left -= u_end - ic.unit;
         next_hk = prm.groups == 1 ? ic.h : ic.h / prm.groups;
-        next_page = next_start + quad < next_len ? paged_page(c, ic.b, next_start + quad) : -1;
-        next_unit(ic, prm, C::kUnit);
+        next_table = c.table + ic.b * c.table_stride;
+        if constexpr (INT8) next_scale = (lane < kQuads ? c.k_scale : c.v_scale) + (static_cast<int64_t>(next_hk) << c.page_shift);
+    };
+    auto prepare = [&]() {
+        while (next_start >= next_end && ic.left > 0) {
+            next_row(ic, prm, unit_shift);
+            if (ic.left > 0) enter_row();
+        }
+        if (next_start >= next_end) return;
+        const int pos = next_start + quad;
+        next_page = -1;
+        if (quad < chunk && pos < ic.len) next_page = next_table[pos >> c.page_shift];
+        if (static_cast<unsigned>(next_page) >= static_cast<unsigned>(c.n_pages)) next_page = -1;
     };
     auto fire = [&]() {
-        if (!next_there) return;
+        if (next_start >= next_end) return;
         const uint32_t bar = ptx::smem_u32(&full_bar[warp][fill]);
-        const uint32_t holes = __ballot_sync(0xffffffffu, next_page < 0 && next_start + quad < next_len);
+        const uint32_t holes = __ballot_sync(0xffffffffu, next_page < 0 && quad < chunk && next_start + quad < ic.len);
         if (lane == 0) hole_s[warp][fill] = holes;
         if (issued != prm.drop_chunk) {
-            const int boxes = (min(CH, next_len - next_start) + (1 << box_shift) - 1) >> box_shift, row = next_start & page_mask;
+            const int boxes = (min(chunk, ic.len - next_start) + (1 << box_shift) - 1) >> box_shift, row = next_start & page_mask;
             if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (boxes << box_shift) * (2 * D * C::kElt));
             const uint32_t dst = ring_u32 + fill * kStageBytes;
 #pragma unroll
             for (int i = 0; i < CH / 16; ++i) {
                 if (i >= boxes) break;
-                // (a hole's box lies outside the map: zeros arrive, nothing is read; more boxes than one: whole pages)
+                // (a hole's box lies outside the map: zeros arrive, nothing is read)
                 const int page = __shfl_sync(0xffffffffu, next_page, i << (box_shift - 2));
                 const uint32_t to = dst + (i << box_shift) * (INT8 ? D : 128);
 #pragma unroll
-                for (int col = 0; col < C::kBoxCols; ++col) {
-                    ptx::tma_load_4d_elect(to + col * (CH * 128), &k_map, bar, col * 64, i == 0 ? row : 0, next_hk, page);
-                    ptx::tma_load_4d_elect(to + col * (CH * 128) + C::kVOff, &v_map, bar, col * 64, i == 0 ? row : 0, next_hk, page);
-                }
+                for (int col = 0; col < C::kBoxCols; ++col)
+                    ptx::tma_load_pair_4d(to + col * (CH * 128), to + col * (CH * 128) + C::kVOff, k_map, v_map, bar, col * 64, (row + (i << box_shift)) & page_mask, next_hk, page);
             }
             if constexpr (INT8) {
-                if (lane < 2 * kQuads) {
-                    const float* from = lane < kQuads ? c.k_scale : c.v_scale;
-                    const int64_t at = ((static_cast<int64_t>(next_page) * c.Hk + next_hk) << c.page_shift) + ((next_start + quad) & page_mask);
-                    ptx::cp_async_16(scale_u32 + fill * (CH * 8) + lane * 16, from + (next_page >= 0 ? at : 0), next_page >= 0);
-                }
+                if (lane < 2 * kQuads)
+                    ptx::cp_async_16(scale_u32 + fill * (CH * 8), next_scale + static_cast<int64_t>(max(next_page, 0)) * page_rows + ((next_start + quad) & page_mask),
+                                     next_page >= 0);
                 ptx::cp_async_arrive(bar);
             }
         }
         ++issued;
         if (++fill == kStages) fill = 0;
+        next_start += unit_keys;
         prepare();
     };
     // Bounded wait for the chunk in `stage`.
@@ -341,28 +411,32 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             if ((++spins & 63u) == 0u && ptx::globaltimer_ns() - begin > prm.wait_limit_ns) return false;
         return true;
     };
-    prepare();
+    if (ic.left > 0) {
+        enter_row();
+        prepare();
+    }
 #pragma unroll 1
     for (int i = 0; i < kStages; ++i) fire();
 
     // ==================================================================== products
-    // What the joining kernel finds for this CTA: the first CTA that begins inside a row joins that row.
-    if (tid == 0) {
+    // What the joining kernel finds: the first worker that begins inside a row has that row joined.
+    if (member == 0 && lane == 0) {
+        const int worker = work.worker;
         int4 job = make_int4(-1, 0, 0, 0);
         if (cc.left > 0 && cc.unit > 0) {
-            const int first = static_cast<int>(static_cast<int64_t>(cta) * total / used);
-            const int before = static_cast<int>(static_cast<int64_t>(cta - 1) * total / used);
-            if (before <= first - cc.unit) {
-                const int64_t end = static_cast<int64_t>(first) - cc.unit + cc.n_units;         // of the row
-                const int last = static_cast<int>((end * used - 1) / total);                    // CTA with the row's last unit
-                // sequence, row, the slot of the part in front, parts of this CTA and those behind it
-                job = make_int4(cc.b, cc.h, 2 * (cta - 1) + (before == first - cc.unit ? 0 : 1), last - cta + 1);
+            const int row_first = work.first_of(worker) - cc.unit, before = work.first_of(worker - 1);
+            if (before <= row_first) {
+                const int last = work.worker_of(row_first + cc.n_units - 1);
+                // row, the slot of the part in front, and the workers whose first slots hold the others
+                job = make_int4(cc.b * prm.HG + cc.h, 2 * (worker - 1) + (before == row_first ? 0 : 1), worker, last - worker + 1);
             }
         }
-        prm.join[cta] = job;
+        if (!prm.jobs_by_row) prm.join[blockIdx.x * (W / C::kMinTeam) + team_no] = job;
+        else if (job.x >= 0) prm.join[job.x] = job;
     }
+    if (!prm.jobs_by_row && tid > 0 && tid < W / C::kMinTeam && tid >= W / team) prm.join[blockIdx.x * (W / C::kMinTeam) + tid] = make_int4(-1, 0, 0, 0);
     // sequences without a key
-    for (int b = cta; b < c.B; b += gridDim.x) {
+    for (int b = blockIdx.x; b < c.B; b += gridDim.x) {
         if (paged_len(c, b) > 0) continue;
         for (int i = tid; i < prm.Hq * (D / 8); i += 32 * W) {
             const int hq = i / (D / 8);
@@ -370,75 +444,62 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
         }
         if (prm.lse != nullptr)
             for (int hq = tid; hq < prm.Hq; hq += 32 * W) prm.lse[static_cast<int64_t>(b) * prm.Hq + hq] = -INFINITY;
+        if (prm.jobs_by_row)
+            for (int h = tid; h < prm.HG; h += 32 * W) prm.join[b * prm.HG + h] = make_int4(-1, 0, 0, 0);
     }
 
-    const float* scale_ring = reinterpret_cast<const float*>(ring + kRingBytes) + warp * (kStages * CH * 2);
+    const float* const scale_ring = reinterpret_cast<const float*>(ring + C::kRingBytes) + warp * (kStages * CH * 2);
+    // Where this lane's pieces of a stage lie.  INT8: rows key_of_row(g) of the keys, key_of_row(2 t) and (2 t + 1) of the
+    // values; the other rows of a block are 8 or 16 rows, the other half of a row of 128 is bit 6 away.
+    const int k_row = key_of_row<D>(g), v_row0 = key_of_row<D>(2 * t), v_row1 = key_of_row<D>(2 * t + 1);
+    const uint8_t* const stages = ring + warp * (kStages * kStageBytes);
+    const uint32_t k_at = code_piece<D>(k_row, t);
+    const uint32_t v_at0 = C::kVOff + (D == 128 ? code_piece<D>(v_row0, g) : code_piece<D>(v_row0, g >> 1) + 8 * (g & 1));
+    const uint32_t v_at1 = C::kVOff + (D == 128 ? code_piece<D>(v_row1, g) : code_piece<D>(v_row1, g >> 1) + 8 * (g & 1));
     int stage = 0, taken = 0;
     uint32_t phase = 0u;
     bool failed = false, first_segment = true;      // failed: a wait ran out; no more copies, the rows from here on are NaN
 #pragma unroll 1
     while (cc.left > 0) {
-        // ------------------------------------------------ a row, or this CTA's part of it
+        // ------------------------------------------------ a row, or this worker's part of it
         const int u_end = min(cc.n_units, cc.unit + cc.left);
-        const int hk = cc.h / prm.groups, q_first = (cc.h - hk * prm.groups) * 8 * NB;
-
-        // ---- query fragments: the right operand (columns = heads g of the block), and what a score is multiplied by
-        uint32_t qf[NB][D / 16][2];
-        float q_mul[NB][2];
+        float q_mul[NB][2];                                   // what a score is multiplied by
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const bool on = q_first + 8 * nb + g < prm.R;
-            const uint8_t* row = prm.q + cc.b * prm.qs[0] + (static_cast<int64_t>(hk) * prm.R + q_first + 8 * nb + g) * prm.qs[1];
             q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
-            if constexpr (INT8) {
-                // fragment 4 j + w holds features 16 (t + 4 j) + 4 w .. + 3, as the codes come
-#pragma unroll
-                for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if (on) x = __ldcg(reinterpret_cast<const uint4*>(row + 32 * (t + 4 * j)) + i);
-                        qf[nb][4 * j + 2 * i][0] = x.x; qf[nb][4 * j + 2 * i][1] = x.y;
-                        qf[nb][4 * j + 2 * i + 1][0] = x.z; qf[nb][4 * j + 2 * i + 1][1] = x.w;
-                    }
-                if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-                    // bfloat16 queries as FP16: multiplied by the power of two that brings the row's largest value to
-                    // [2^13, 2^14); eight mantissa bits fit, and what becomes subnormal is below 2^-27 of the largest
-                    uint32_t top = 0u;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t a = qf[nb][i][k] & 0x7fff7fffu;
-                            top = max(top, max(a & 0xffffu, a >> 16));
-                        }
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const uint32_t e = top == 0u ? 140u : max(top >> 7, 14u);
-                    const float up = __uint_as_float((267u - e) << 23), down = __uint_as_float((e - 13u) << 23);
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float2 f = act_to_float2(qf[nb][i][k], __nv_bfloat16());
-                            qf[nb][i][k] = act_pack2(f.x * up, f.y * up, __half());
-                        }
-                    q_mul[nb][0] *= __shfl_sync(0xffffffffu, down, 8 * t);
-                    q_mul[nb][1] *= __shfl_sync(0xffffffffu, down, 8 * t + 4);
-                }
-            } else {
+            if constexpr (INT8 && std::is_same<T, __nv_bfloat16>::value) {
+                // bfloat16 queries as FP16: multiplied by the power of two that brings the row's largest value to
+                // [2^13, 2^14); eight mantissa bits fit, and what becomes subnormal is below 2^-27 of the largest
+                uint32_t top = 0u;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        qf[nb][i][k] = on ? __ldcg(reinterpret_cast<const uint32_t*>(row + 32 * i + 16 * k) + t) : 0u;
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t a = qf[nb][i][k] & 0x7fff7fffu;
+                        top = max(top, max(a & 0xffffu, a >> 16));
+                    }
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const uint32_t e = top == 0u ? 140u : max(top >> 7, 14u);
+                const float up = __uint_as_float((267u - e) << 23), down = __uint_as_float((e - 13u) << 23);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float2 f = act_to_float2(qf[nb][i][k], __nv_bfloat16());
+                        qf[nb][i][k] = act_pack2(f.x * up, f.y * up, __half());
+                    }
+                q_mul[nb][0] *= __shfl_sync(0xffffffffu, down, 8 * t);
+                q_mul[nb][1] *= __shfl_sync(0xffffffffu, down, 8 * t + 4);
             }
         }
 
-        float m_run[NB][2], z[NB][2], acc[D / 16][NB][4];
+        // sub = kOff less the running maximum, which is rounded up to a whole number: exponents lose nothing by it, and what
+        // has been summed is brought to another maximum exactly.
+        float sub[NB][2], z[NB][2], acc[D / 16][NB][4];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            m_run[nb][0] = m_run[nb][1] = kNoMax;
+            sub[nb][0] = sub[nb][1] = C::kOff - kNoMax;
             z[nb][0] = z[nb][1] = 0.f;
 #pragma unroll
             for (int md = 0; md < D / 16; ++md) acc[md][nb][0] = acc[md][nb][1] = acc[md][nb][2] = acc[md][nb][3] = 0.f;
@@ -446,17 +507,18 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
         // INT8: the scale of a value is folded into its probability relative to v_ref, a power of two at or above every
         // scale so far; O~ is in units of it.
         float v_ref = 7.888609052210118e-31f;                 // 2^-100
-        const int end = min(cc.len, u_end * C::kUnit);        // keys of this segment
+        const int end = min(cc.len, u_end << unit_shift);       // keys of this segment
         bool any = false;
         int held = 0;
 
 #pragma unroll 1
-        for (int start = (cc.unit * W + warp) * CH; start < end; start += C::kUnit) {
+        for (int start = (cc.unit << unit_shift) + (member << chunk_shift); start < end; start += unit_keys) {
             if (!failed && !landed(stage, phase)) failed = true;
             if (failed) break;
             any = true;
             const uint32_t kst = ring_u32 + stage * kStageBytes, vst = kst + C::kVOff;
-            const int live = min(CH, cc.len - start);         // keys of the chunk
+            const uint8_t* const st = stages + stage * kStageBytes;
+            const int live = min(chunk, cc.len - start), blocks = (live + 15) >> 4;        // keys of the chunk
             const uint32_t holes = hole_s[warp][stage];
             const bool partial = live < CH || holes != 0u;
             // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same)
@@ -465,11 +527,12 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) sc[mb][nb][0] = sc[mb][nb][1] = sc[mb][nb][2] = sc[mb][nb][3] = 0.f;
+                if (MB > 1 && mb >= blocks) continue;
                 if constexpr (INT8) {
-                    const int r0 = 16 * mb + key_of_row<D>(g);
 #pragma unroll
                     for (int j = 0; j < D / 64; ++j) {
-                        const uint4 xa = lds128(kst + code_piece<D>(r0, t + 4 * j)), xb = lds128(kst + code_piece<D>(r0 + 8, t + 4 * j));
+                        const uint8_t* const at = st + (k_at ^ (64 * j)) + 16 * mb * D;
+                        const uint4 xa = *reinterpret_cast<const uint4*>(at), xb = *reinterpret_cast<const uint4*>(at + 8 * D);
                         const uint32_t wa[4] = {xa.x, xa.y, xa.z, xa.w}, wb[4] = {xb.x, xb.y, xb.z, xb.w};
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
@@ -481,7 +544,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
                                 mma_16816<false>(sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
                         }
                     }
-                    const float* sk = scale_ring + stage * (CH * 2) + r0;
+                    const float* sk = scale_ring + stage * (CH * 2) + 16 * mb + k_row;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const float dk = sk[8 * i];
@@ -532,7 +595,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], C::kOff - m_run[nb][k & 1]);
+                        for (int k = 0; k < 4; ++k) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]);
             };
             float e[MB][NB][4];
             exponents(e);
@@ -559,9 +622,9 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                        const float m_new = fmaxf(m_run[nb][k], x * q_mul[nb][k]);
-                        alpha[nb][k] = exp2f(m_run[nb][k] - m_new);
-                        m_run[nb][k] = m_new;
+                        const float s_new = fminf(sub[nb][k], C::kOff - ceilf(x * q_mul[nb][k]));
+                        alpha[nb][k] = exp2f(s_new - sub[nb][k]);
+                        sub[nb][k] = s_new;
                         z[nb][k] *= alpha[nb][k];
                     }
                 if constexpr (INT8) {
@@ -590,6 +653,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             // ---- probabilities, and O^T += V^T P^T block by block
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
+                if (MB > 1 && mb >= blocks) continue;
                 uint32_t p0[NB], p1[NB];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
@@ -606,16 +670,15 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
                 }
                 if constexpr (INT8) {
                     // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
-                    const int r0 = 16 * mb + key_of_row<D>(2 * t), r1 = 16 * mb + key_of_row<D>(2 * t + 1);
                     uint32_t x[4][D / 32];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int row = (i & 1 ? r1 : r0) + (i >> 1) * 8;
+                        const uint8_t* const at = st + (i & 1 ? v_at1 : v_at0) + (16 * mb + 8 * (i >> 1)) * D;
                         if constexpr (D == 128) {
-                            const uint4 v = lds128(vst + code_piece<D>(row, g));
+                            const uint4 v = *reinterpret_cast<const uint4*>(at);
                             x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
                         } else {
-                            const uint2 v = lds64(vst + code_piece<D>(row, g >> 1) + 8 * (g & 1));
+                            const uint2 v = *reinterpret_cast<const uint2*>(at);
                             x[i][0] = v.x; x[i][1] = v.y;
                         }
                     }
@@ -649,12 +712,25 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
             ++taken;
             __syncwarp();                    // every lane is done with the stage; the segment's last one is kept for the merge
-            if (start + C::kUnit < end) fire();
+            if (start + unit_keys < end) fire();
         }
 
         // ------------------------------------------------ the warps' results of the segment, merged in the stages read last
         // (every warp holds the same places of O^T; a warp without a chunk here has no stage to itself: its place is not read)
+        const bool whole = cc.unit == 0 && u_end == cc.n_units;
+        const int slot = 2 * work.worker + (first_segment ? 0 : 1), b = cc.b, h = cc.h;
+        if (whole && prm.jobs_by_row && member == 0 && lane == 0) prm.join[b * prm.HG + h] = make_int4(-1, 0, 0, 0);
+        first_segment = false;
+        cc.left -= u_end - cc.unit;
+        if (cc.left > 0) {
+            next_row(cc, prm, unit_shift);
+            if (cc.left > 0) fetch_q(cc);                     // (on the way during the merge)
+        }
         float4* mine = reinterpret_cast<float4*>(ring + (warp * kStages + held) * kStageBytes);
+        if (lane == 0) {
+            v_ref_s[warp] = any && !failed ? (INT8 ? v_ref : 1.f) : -1.f;
+            held_s[warp] = held;
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -663,58 +739,37 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
                 z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 4);
                 z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 8);
                 z[nb][k] += __shfl_xor_sync(0xffffffffu, z[nb][k], 16);
-                if (g == 0) { m_s[warp][8 * nb + 2 * t + k] = m_run[nb][k]; z_s[warp][8 * nb + 2 * t + k] = z[nb][k]; }
+                if (g == 0) { m_s[warp][8 * nb + 2 * t + k] = C::kOff - sub[nb][k]; z_s[warp][8 * nb + 2 * t + k] = z[nb][k]; }
             }
             if (any && !failed)
 #pragma unroll
                 for (int md = 0; md < D / 16; ++md)
-                    mine[(md * NB + nb) * 32 + lane] = make_float4(acc[md][nb][0], acc[md][nb][1], acc[md][nb][2], acc[md][nb][3]);
-        }
-        if (lane == 0) {
-            v_ref_s[warp] = any && !failed ? (INT8 ? v_ref : 1.f) : -1.f;
-            held_s[warp] = held;
-        }
-        __syncthreads();
-        {
-            const bool whole = cc.unit == 0 && u_end == cc.n_units;
-            const int slot = 2 * cta + (first_segment ? 0 : 1);
+                    mine[md * 32 + lane] = make_float4(acc[md][nb][0], acc[md][nb][1], acc[md][nb][2], acc[md][nb][3]);
+            team_sync();
+            const int w0 = warp - member, n = 8 * nb + 2 * t;
+            float m[2] = {m_s[w0][n], m_s[w0][n + 1]};
+            for (int w = w0 + 1; w < w0 + team; ++w) { m[0] = fmaxf(m[0], m_s[w][n]); m[1] = fmaxf(m[1], m_s[w][n + 1]); }
 #pragma unroll 1
-            for (int i = warp; i < (D / 16) * NB; i += W) {
-                const int md = i / NB, nb = i - md * NB;
-                float m[2], zz[2], wgt[W][2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int n = 8 * nb + 2 * t + k;
-                    m[k] = m_s[0][n];
-#pragma unroll
-                    for (int w = 1; w < W; ++w) m[k] = fmaxf(m[k], m_s[w][n]);
-                    zz[k] = 0.f;
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        const float f = exp2f(m_s[w][n] - m[k]) * C::kUnOff;
-                        zz[k] += z_s[w][n] * f;
-                        wgt[w][k] = f * v_ref_s[w];
-                    }
-                }
+            for (int md = member; md < D / 16; md += team) {
+                float zz[2] = {0.f, 0.f};
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    if (v_ref_s[w] < 0.f) continue;
-                    const float4 x = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes)[i * 32 + lane];
-                    o.x += x.x * wgt[w][0]; o.y += x.y * wgt[w][1]; o.z += x.z * wgt[w][0]; o.w += x.w * wgt[w][1];
+#pragma unroll 4
+                for (int w = w0; w < w0 + team; ++w) {
+                    const float f0 = exp2f(m_s[w][n] - m[0]) * C::kUnOff, f1 = exp2f(m_s[w][n + 1] - m[1]) * C::kUnOff, ref = v_ref_s[w];
+                    zz[0] += z_s[w][n] * f0; zz[1] += z_s[w][n + 1] * f1;
+                    if (ref < 0.f) continue;
+                    const float4 x = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes)[md * 32 + lane];
+                    o.x += x.x * (f0 * ref); o.y += x.y * (f1 * ref); o.z += x.z * (f0 * ref); o.w += x.w * (f1 * ref);
                 }
-                if (whole) write_out<T, D, INT8, NB>(prm, cc.b, cc.h, md, nb, lane, o, m, zz);
-                else prm.part_o[static_cast<int64_t>(slot) * C::kFrag + i * 32 + lane] = o;
+                if (whole) write_out<T, D, INT8, NB>(prm, b, h, md, nb, lane, o, m, zz);
+                else prm.part_o[(static_cast<int64_t>(slot) * NB + nb) * C::kFrag + md * 32 + lane] = o;
                 if (!whole && md == 0 && g == 0)
-                    *reinterpret_cast<float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t) = make_float4(m[0], zz[0], m[1], zz[1]);
+                    *reinterpret_cast<float4*>(prm.part_mz + slot * (8 * NB) + n) = make_float4(m[0], zz[0], m[1], zz[1]);
             }
+            if (nb == NB - 1) ptx::fence_proxy_async_smem();  // the stages go back to the copies
+            team_sync();
         }
-        ptx::fence_proxy_async_smem();       // the stages go back to the copies
-        __syncthreads();
         if (any && !failed) fire();
-        first_segment = false;
-        cc.left -= u_end - cc.unit;
-        if (cc.left > 0) next_row(cc, prm, C::kUnit);
     }
     if (failed) {
         // the copies that are still on the way land before the shared memory is given back
@@ -727,84 +782,92 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ CUtenso
     }
 }
 
-// Joins the parts of a row that several CTAs shared: job (b, h, s, n) of the CTA blockIdx.x names slot s and, of that CTA and
-// the n - 1 behind it, their first slots.  Block y takes rows md = y of the fragments; its warps take the parts in turn and
-// several at a time (what bounds it is the round trips), then merge in shared memory.
-constexpr int kJoinWarps = 8, kJoinAtOnce = 4;
+// Joins the parts of the rows that several workers shared.  A job (row, s, w, n) names slot s and the first slots of n workers
+// from w on.  What bounds it is the round trips: the parts are loaded eight at a time.  A row of up to eight parts has a warp
+// for every fragment; the parts of others are shared out over the warps, fragment by fragment (by a block each where rows are few).
+constexpr int kJoinWarps = 8, kJoinAtOnce = 8;
 template <class T, int D, bool INT8, int NB>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 paged_join_kernel(const PagedDecodeParams prm) {
-    __shared__ float4 o_s[kJoinWarps][NB][32];
-    __shared__ float2 mz_s[kJoinWarps][NB][32][2];
+    using C = Cfg<T, D, INT8, NB>;
+    __shared__ float4 o_s[kJoinWarps][32];
+    __shared__ float4 mz_s[kJoinWarps][32];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    using C = Cfg<T, D, INT8, NB>;
     const int4 job = __ldcg(prm.join + blockIdx.x);
     if (job.x < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, md = blockIdx.y, parts = job.w + 1;
-    float4 o[NB];
-    float m[NB][2], z[NB][2];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        o[nb] = make_float4(0.f, 0.f, 0.f, 0.f);
-        m[nb][0] = m[nb][1] = kNoMax;
-        z[nb][0] = z[nb][1] = 0.f;
-    }
-    auto add = [&](int nb, const float4& x, const float2 (&mz)[2]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, parts = job.w + 1;
+    const int b = job.x / prm.HG, h = job.x - b * prm.HG;
+    constexpr int F = (D / 16) * NB;
+    const int f_begin = blockIdx.y * F / gridDim.y, f_end = (blockIdx.y + 1) * F / gridDim.y;
+
+    float4 o;
+    float m[2], z[2];
+    auto clear = [&]() {
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        m[0] = m[1] = kNoMax;
+        z[0] = z[1] = 0.f;
+    };
+    auto add = [&](const float4& x, const float4& mz) {
         float back[2], fore[2];
+        const float mm[2] = {mz.x, mz.z}, zz[2] = {mz.y, mz.w};
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const float top = fmaxf(m[nb][k], mz[k].x);
-            back[k] = exp2f(m[nb][k] - top);
-            fore[k] = exp2f(mz[k].x - top);
-            z[nb][k] = z[nb][k] * back[k] + mz[k].y * fore[k];
-            m[nb][k] = top;
+            const float top = fmaxf(m[k], mm[k]);
+            back[k] = exp2f(m[k] - top);
+            fore[k] = exp2f(mm[k] - top);
+            z[k] = z[k] * back[k] + zz[k] * fore[k];
+            m[k] = top;
         }
-        o[nb].x = o[nb].x * back[0] + x.x * fore[0]; o[nb].y = o[nb].y * back[1] + x.y * fore[1];
-        o[nb].z = o[nb].z * back[0] + x.z * fore[0]; o[nb].w = o[nb].w * back[1] + x.w * fore[1];
+        o.x = o.x * back[0] + x.x * fore[0]; o.y = o.y * back[1] + x.y * fore[1];
+        o.z = o.z * back[0] + x.z * fore[0]; o.w = o.w * back[1] + x.w * fore[1];
     };
-    for (int i0 = warp; i0 < parts; i0 += kJoinWarps * kJoinAtOnce) {
-        float4 x[kJoinAtOnce][NB];
-        float2 mz[kJoinAtOnce][NB][2];
+    // parts first, first + step, ... of fragment f = nb D / 16 + md
+    auto add_parts = [&](int f, int first, int step) {
+        const int nb = f / (D / 16);
+        for (int i0 = first; i0 < parts; i0 += step * kJoinAtOnce) {
+            float4 x[kJoinAtOnce], mz[kJoinAtOnce];
 #pragma unroll
-        for (int j = 0; j < kJoinAtOnce; ++j) {
-            const int i = i0 + j * kJoinWarps;
-            if (i >= parts) continue;
-            const int64_t slot = i == 0 ? job.z : 2 * (static_cast<int>(blockIdx.x) + i - 1);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                x[j][nb] = __ldcg(prm.part_o + slot * C::kFrag + (md * NB + nb) * 32 + lane);
-                const float4 two = __ldcg(reinterpret_cast<const float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t));
-                mz[j][nb][0] = make_float2(two.x, two.y);
-                mz[j][nb][1] = make_float2(two.z, two.w);
+            for (int j = 0; j < kJoinAtOnce; ++j) {
+                const int i = i0 + j * step;
+                if (i >= parts) continue;
+                const int64_t slot = i == 0 ? job.y : 2 * (job.z + i - 1);
+                x[j] = __ldcg(prm.part_o + slot * (NB * C::kFrag) + f * 32 + lane);
+                mz[j] = __ldcg(reinterpret_cast<const float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t));
             }
+#pragma unroll
+            for (int j = 0; j < kJoinAtOnce; ++j)
+                if (i0 + j * step < parts) add(x[j], mz[j]);
         }
-#pragma unroll
-        for (int j = 0; j < kJoinAtOnce; ++j)
-            if (i0 + j * kJoinWarps < parts)
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) add(nb, x[j][nb], mz[j][nb]);
+    };
+    if (parts <= kJoinAtOnce) {
+        for (int f = f_begin + warp; f < f_end; f += kJoinWarps) {
+            clear();
+            add_parts(f, 0, 1);
+            write_out<T, D, INT8, NB>(prm, b, h, f % (D / 16), f / (D / 16), lane, o, m, z);
+        }
+        return;
     }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        o_s[warp][nb][lane] = o[nb];
-        mz_s[warp][nb][lane][0] = make_float2(m[nb][0], z[nb][0]);
-        mz_s[warp][nb][lane][1] = make_float2(m[nb][1], z[nb][1]);
+    for (int f = f_begin; f < f_end; ++f) {
+        clear();
+        add_parts(f, warp, kJoinWarps);
+        o_s[warp][lane] = o;
+        mz_s[warp][lane] = make_float4(m[0], z[0], m[1], z[1]);
+        __syncthreads();
+        if (warp == 0) {
+            for (int w = 1; w < kJoinWarps; ++w) add(o_s[w][lane], mz_s[w][lane]);
+            write_out<T, D, INT8, NB>(prm, b, h, f % (D / 16), f / (D / 16), lane, o, m, z);
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    if (warp >= NB) return;
-    const int nb = warp;
-    o[0] = o_s[0][nb][lane];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) { m[0][k] = mz_s[0][nb][lane][k].x; z[0][k] = mz_s[0][nb][lane][k].y; }
-    for (int w = 1; w < min(kJoinWarps, parts); ++w) add(0, o_s[w][nb][lane], mz_s[w][nb][lane]);
-    write_out<T, D, INT8, NB>(prm, job.x, job.y, md, nb, lane, o[0], m[0], z[0]);
 }
 
 // ---------------------------------------------------------------------------------------------------- host
 
+// Shape of a launch by instance: what resolve_decode has to know of Cfg.
 struct Plan {
-    int NB, groups, HG, unit, ctas, splits;      // splits: whether a row can have more units than one
+    int NB, groups, HG, ctas, jobs, splits;      // splits: whether a row can have more units than one
+    int team, workers;                           // smallest team; workers that there may be
     size_t join_bytes, mz_bytes, total;
 };
 
@@ -815,16 +878,33 @@ int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* p
     const int R = heads_q / p->heads_kv;
     plan->NB = R > 8 ? 2 : 1;
     plan->groups = static_cast<int>(ceil_div(R, 8 * plan->NB));
-    plan->unit = kRingBytes / kStages / (2 * p->head_dim * (p->cache_type == TILEMIX_CACHE_INT8 ? 1 : 2));    // Cfg::kUnit
-    const int64_t rows = static_cast<int64_t>(p->heads_kv) * plan->groups;
-    const int64_t units = rows * p->batch * ceil_div(c->capacity, plan->unit);
-    if (rows > (1 << 24) || units > (int64_t{1} << 30) || static_cast<int64_t>(p->batch) * heads_q > (int64_t{1} << 30)) return TILEMIX_ERR_SHAPE;
-    plan->HG = static_cast<int>(rows);
-    plan->ctas = static_cast<int>(units < kCtasPerSm * kSms ? units : kCtasPerSm * kSms);
-    plan->splits = c->capacity > plan->unit;
-    plan->join_bytes = (plan->ctas * sizeof(int4) + 255) / 256 * 256;
-    plan->mz_bytes = (static_cast<size_t>(plan->ctas) * 2 * 8 * plan->NB * sizeof(float2) + 255) / 256 * 256;
-    plan->total = plan->join_bytes + plan->mz_bytes + static_cast<size_t>(plan->ctas) * 2 * p->head_dim * 8 * plan->NB * sizeof(float);
+    int W, min_team, wave;
+    auto shape = [&](auto cfg) {
+        using C = decltype(cfg);
+        W = C::W; min_team = C::kMinTeam; wave = C::kCtasPerSm * kSms;
+    };
+    const bool int8 = p->cache_type == TILEMIX_CACHE_INT8;
+    if (p->head_dim == 128) {
+        if (int8) { if (plan->NB == 1) shape(Cfg<__half, 128, true, 1>()); else shape(Cfg<__half, 128, true, 2>()); }
+        else { if (plan->NB == 1) shape(Cfg<__half, 128, false, 1>()); else shape(Cfg<__half, 128, false, 2>()); }
+    } else {
+        if (int8) { if (plan->NB == 1) shape(Cfg<__half, 64, true, 1>()); else shape(Cfg<__half, 64, true, 2>()); }
+        else { if (plan->NB == 1) shape(Cfg<__half, 64, false, 1>()); else shape(Cfg<__half, 64, false, 2>()); }
+    }
+    const int64_t rows_each = static_cast<int64_t>(p->heads_kv) * plan->groups;
+    if (rows_each > (1 << 22)) return TILEMIX_ERR_SHAPE;
+    const int64_t rows = rows_each * p->batch;
+    if (rows > (1 << 28) || rows * ceil_div(c->capacity, 16) > (int64_t{1} << 30)) return TILEMIX_ERR_SHAPE;   // (units are counted in 32 bits)
+    if (static_cast<int64_t>(p->batch) * heads_q > (int64_t{1} << 30)) return TILEMIX_ERR_SHAPE;
+    plan->HG = static_cast<int>(rows_each);
+    const int64_t units = rows * ceil_div(c->capacity, 16 * W);       // (the kernel makes chunks as small as 16 keys)
+    plan->ctas = static_cast<int>(units < wave ? units : wave);
+    plan->splits = c->capacity > 16 * min_team;
+    plan->workers = plan->ctas * (W / min_team);
+    plan->jobs = static_cast<int>(rows < plan->workers ? rows : plan->workers);
+    plan->join_bytes = (plan->jobs * sizeof(int4) + 255) / 256 * 256;
+    plan->mz_bytes = (static_cast<size_t>(plan->workers) * 2 * 8 * plan->NB * sizeof(float2) + 255) / 256 * 256;
+    plan->total = plan->join_bytes + plan->mz_bytes + static_cast<size_t>(plan->workers) * 2 * p->head_dim * 8 * plan->NB * sizeof(float);
     return TILEMIX_OK;
 }
 
@@ -848,12 +928,16 @@ template <class T, int D, bool INT8, int NB>
 int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) {
     using C = Cfg<T, D, INT8, NB>;
     const PagedCache& c = prm.c;
-    static_assert(C::kUnit == kRingBytes / kStages / (2 * D * C::kElt), "see resolve_decode");
-    CUtensorMap km, vm;
+    PoolMaps maps;
     const int page = 1 << c.page_shift, box_rows = page < C::CH ? page : C::CH;
     int rc;
-    if ((rc = encode_pool_map(&km, c.k_pool, C::kElt, D, page, c.Hk, c.n_pages, c.ks, box_rows))) return rc;
-    if ((rc = encode_pool_map(&vm, c.v_pool, C::kElt, D, page, c.Hk, c.n_pages, c.vs, box_rows))) return rc;
+    if ((rc = encode_pool_map(&maps.k, c.k_pool, C::kElt, D, page, c.Hk, c.n_pages, c.ks, box_rows))) return rc;
+    if ((rc = encode_pool_map(&maps.v, c.v_pool, C::kElt, D, page, c.Hk, c.n_pages, c.vs, box_rows))) return rc;
+    maps.k16 = maps.k; maps.v16 = maps.v;
+    if (box_rows > 16) {
+        if ((rc = encode_pool_map(&maps.k16, c.k_pool, C::kElt, D, page, c.Hk, c.n_pages, c.ks, 16))) return rc;
+        if ((rc = encode_pool_map(&maps.v16, c.v_pool, C::kElt, D, page, c.Hk, c.n_pages, c.vs, 16))) return rc;
+    }
     auto kernel = paged_decode_kernel<T, D, INT8, NB>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return static_cast<int>(e);
@@ -863,10 +947,11 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, prm, km, vm);
+    e = cudaLaunchKernelEx(&cfg, kernel, prm, maps);
     g_launch_count.fetch_add(1);
     if (e != cudaSuccess || !plan.splits) return static_cast<int>(e);
-    cfg.gridDim = dim3(plan.ctas, D / 16); cfg.blockDim = dim3(32 * kJoinWarps); cfg.dynamicSmemBytes = 0;
+    const int F = (D / 16) * NB;
+    cfg.gridDim = dim3(plan.jobs, prm.jobs_by_row && plan.jobs < plan.ctas ? F : 1); cfg.blockDim = dim3(32 * kJoinWarps); cfg.dynamicSmemBytes = 0;
     e = cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB>, prm);
     g_launch_count.fetch_add(1);
     return static_cast<int>(e);
@@ -913,6 +998,7 @@ int tilemix_paged_decode(const tilemix_paged_t* p, int32_t heads_q, float softma
     prm.join = reinterpret_cast<int4*>(ws);
     prm.part_mz = reinterpret_cast<float2*>(ws + plan.join_bytes);
     prm.part_o = reinterpret_cast<float4*>(ws + plan.join_bytes + plan.mz_bytes);
+    prm.jobs_by_row = static_cast<int64_t>(plan.HG) * p->batch <= plan.workers ? 1 : 0;
     prm.wait_limit_ns = g_wait_limit_ns.load();
     prm.drop_chunk = g_test_drop.load() == 2 ? 1 : -1;
     const bool int8 = p->cache_type == TILEMIX_CACHE_INT8;

@@ -82,13 +82,15 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
         : "memory");
 }
 
-// The same by a whole, converged warp with warp-uniform arguments; one elected lane issues the copy.
-__device__ __forceinline__ void tma_load_4d_elect(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
+// Two loads with the same coordinates, by a whole, converged warp with warp-uniform arguments; one elected lane issues them.
+__device__ __forceinline__ void tma_load_pair_4d(uint32_t dst_a, uint32_t dst_b, const CUtensorMap* tm_a, const CUtensorMap* tm_b,
+                                                 uint32_t bar, int c0, int c1, int c2, int c3) {
     asm volatile(
         "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-        "@e cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%3, %4, %5, %6}], [%2];\n\t}"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        "@e cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%2, {%5, %6, %7, %8}], [%4];\n\t"
+        "@e cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%1], [%3, {%5, %6, %7, %8}], [%4];\n\t}"
+        ::"r"(dst_a), "r"(dst_b), "l"(reinterpret_cast<uint64_t>(tm_a)), "l"(reinterpret_cast<uint64_t>(tm_b)), "r"(bar),
+        "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
 
