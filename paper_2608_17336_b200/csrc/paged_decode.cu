@@ -189,16 +189,21 @@ template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE>
 __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     constexpr int kTeamShift = W == 8 ? 3 : 2, kMinShift = MIN_TEAM == 2 ? 1 : 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = prm.c.B, ctas = gridDim.x;
-    const int len0 = lane < B ? paged_len(prm.c, lane) : 0;
-    auto len_of = [&](int b) { return b < 32 ? len0 : b < B ? paged_len(prm.c, b) : 0; };
-    int blocks = 0, rows = 0;                // of 16 keys; sequences with a key
-    for (int b = lane; b < B; b += 32) {
-        const int len = len_of(b);
-        blocks += (len + 15) >> 4;
-        rows += len > 0 ? 1 : 0;
-    }
-    blocks = __reduce_add_sync(0xffffffffu, blocks) * prm.HG;
-    rows = __reduce_add_sync(0xffffffffu, rows) * prm.HG;
+    // (the lengths of the first 256 sequences stay in registers: the loads wait for memory once)
+    constexpr int kKept = 8;
+    int kept[kKept];
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) kept[i] = lane + 32 * i < B ? paged_len(prm.c, lane + 32 * i) : 0;
+    // sum of f(length) over the sequences, of this lane
+    auto sum_of = [&](auto f) {
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) sum += f(kept[i]);
+        for (int b = 32 * kKept + lane; b < B; b += 32) sum += f(paged_len(prm.c, b));
+        return sum;
+    };
+    const int blocks = __reduce_add_sync(0xffffffffu, sum_of([](int len) { return (len + 15) >> 4; })) * prm.HG;     // of 16 keys
+    const int rows = __reduce_add_sync(0xffffffffu, sum_of([](int len) { return len > 0 ? 1 : 0; })) * prm.HG;
     Work w{};
     w.team_shift = kTeamShift; w.chunk_shift = CH_SHIFT;
     while (w.chunk_shift > 4 && (blocks >> (w.chunk_shift - 4 + kTeamShift)) < ctas) --w.chunk_shift;
@@ -206,74 +211,88 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
            (blocks >> (w.chunk_shift - 4 + w.team_shift)) < kShortRow * rows)
         --w.team_shift;
     const int unit_shift = w.chunk_shift + w.team_shift;
-    int sum = 0;
-    for (int b = lane; b < B; b += 32) sum += (len_of(b) + (1 << unit_shift) - 1) >> unit_shift;
-    const int U = __reduce_add_sync(0xffffffffu, sum) * prm.HG, n = min(ctas << (kTeamShift - w.team_shift), U);
+    auto units_of = [&](int len) { return (len + (1 << unit_shift) - 1) >> unit_shift; };
+    const int U = __reduce_add_sync(0xffffffffu, sum_of(units_of)) * prm.HG, n = min(ctas << (kTeamShift - w.team_shift), U);
     w.worker = (blockIdx.x << (kTeamShift - w.team_shift)) + (warp >> w.team_shift);
     if (w.worker >= n) return w;
     w.base = U / n; w.longer = U - w.base * n;
     Cursor& c = w.at;
     const int first = w.first_of(w.worker);
     int before = 0;                          // units of the sequences before the 32 in hand
-    for (int b0 = 0; b0 < B; b0 += 32) {
-        const int len = len_of(b0 + lane), mine = (len + (1 << unit_shift) - 1) >> unit_shift;
+    auto among = [&](int b0, int len) -> bool {
+        const int mine = units_of(len), all = __reduce_add_sync(0xffffffffu, mine) * prm.HG;
+        if (before + all <= first) {
+            before += all;
+            return false;
+        }
         int upto = mine * prm.HG;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += x;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, before + upto > first);
-        if (past != 0u) {
-            const int l = __ffs(past) - 1;
-            c.b = b0 + l;
-            c.n_units = __shfl_sync(0xffffffffu, mine, l);
-            c.len = __shfl_sync(0xffffffffu, len, l);
-            const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - c.n_units * prm.HG);
-            c.h = at / c.n_units;
-            c.unit = at - c.h * c.n_units;
-            c.left = w.base + (w.worker < w.longer ? 1 : 0);
-            return w;
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
-    }
+        const int l = __ffs(__ballot_sync(0xffffffffu, before + upto > first)) - 1;
+        c.b = b0 + l;
+        c.n_units = __shfl_sync(0xffffffffu, mine, l);
+        c.len = __shfl_sync(0xffffffffu, len, l);
+        const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - c.n_units * prm.HG);
+        c.h = at / c.n_units;
+        c.unit = at - c.h * c.n_units;
+        c.left = w.base + (w.worker < w.longer ? 1 : 0);
+        return true;
+    };
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+        if (32 * i < B && among(32 * i, kept[i])) return w;
+    for (int b0 = 32 * kKept; b0 < B; b0 += 32)
+        if (among(b0, b0 + lane < B ? paged_len(prm.c, b0 + lane) : 0)) return w;
     return w;
 }
 
 // ---------------------------------------------------------------------------------------------------- results
-// Fragment (md, lane) of O^T: x, y = row d0 of query columns 2 t, 2 t + 1; z, w = row d1; (d0, d1) = (16 md + g, + 8), of an
-// INT8 cache (D / 8 g + 2 md, + 1).
-__device__ __forceinline__ uint8_t* out_row(const PagedDecodeParams& prm, int b, int h, int width, int n) {
-    const int hk = h / prm.groups, first = (h - hk * prm.groups) * width;
-    return first + n < prm.R ? prm.out + b * prm.os[0] + (static_cast<int64_t>(hk) * prm.R + first + n) * prm.os[1] : nullptr;
-}
+// Where the rows of query columns 2 t, 2 t + 1 of block nb go, and what their sums are divided by.  Fragment (md, lane) of O^T
+// is (d0, column 2 t), (d0, 2 t + 1), (d1, 2 t), (d1, 2 t + 1) with (d0, d1) = (16 md + g, + 8), of an INT8 cache
+// (D / 8 g + 2 md, + 1).
+template <class T, int D, bool INT8>
+struct OutRows {
+    uint8_t* dst[2];                // nullptr: there is no such query head
+    float inv[2];
 
-// Writes the normalised fragment of query columns 2 t, 2 t + 1 of block nb, and the row's lse with fragment 0.
-template <class T, int D, bool INT8, int NB>
-__device__ __forceinline__ void write_out(const PagedDecodeParams& prm, int b, int h, int md, int nb, int lane, const float4& o,
-                                          const float (&m)[2], const float (&z)[2]) {
-    const int g = lane >> 2, t = lane & 3;
-    const float v[2][2] = {{o.x, o.z}, {o.y, o.w}};
+    __device__ __forceinline__ OutRows(const PagedDecodeParams& prm, int b, int h, int width, int nb, int lane) {
+        const int hk = prm.groups == 1 ? h : h / prm.groups, n = (h - hk * prm.groups) * width + 8 * nb + 2 * (lane & 3);
+        uint8_t* row = prm.out + b * prm.os[0] + (static_cast<int64_t>(hk) * prm.R + n) * prm.os[1];
+        dst[0] = n < prm.R ? row : nullptr;
+        dst[1] = n + 1 < prm.R ? row + prm.os[1] : nullptr;
+        head = static_cast<int64_t>(b) * prm.Hq + hk * prm.R + n;
+    }
+    // Sums of the columns; the lse of their rows by the lanes of `write_lse`.
+    __device__ __forceinline__ void sums(const PagedDecodeParams& prm, const float (&m)[2], const float (&z)[2], bool write_lse) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int n = 8 * nb + 2 * t + i;
-        uint8_t* dst = out_row(prm, b, h, 8 * NB, n);
-        if (dst == nullptr) continue;
-        const bool empty = z[i] == 0.f;
-        const uint32_t two = act_pack2(empty ? 0.f : v[i][0] / z[i], empty ? 0.f : v[i][1] / z[i], T());
-        if constexpr (INT8) {
-            reinterpret_cast<uint32_t*>(dst)[(D / 16) * g + md] = two;
-        } else {
-            reinterpret_cast<uint16_t*>(dst)[16 * md + g] = static_cast<uint16_t>(two);
-            reinterpret_cast<uint16_t*>(dst)[16 * md + g + 8] = static_cast<uint16_t>(two >> 16);
-        }
-        if (md == 0 && g == 0 && prm.lse != nullptr) {
-            const int hk = h / prm.groups;
-            prm.lse[static_cast<int64_t>(b) * prm.Hq + hk * prm.R + (h - hk * prm.groups) * 8 * NB + n] =
-                empty ? -INFINITY : (m[i] + log2f(z[i])) * kLn2;
+        for (int i = 0; i < 2; ++i) {
+            const bool empty = z[i] == 0.f;              // (not if it is a NaN)
+            inv[i] = empty ? 0.f : __fdividef(1.f, z[i]);
+            if (write_lse && dst[i] != nullptr && prm.lse != nullptr) prm.lse[head + i] = empty ? -INFINITY : (m[i] + log2f(z[i])) * kLn2;
         }
     }
-}
+    __device__ __forceinline__ void store(int md, int lane, const float4& o) const {
+        const int g = lane >> 2;
+        const float v[2][2] = {{o.x, o.z}, {o.y, o.w}};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (dst[i] == nullptr) continue;
+            const uint32_t two = act_pack2(v[i][0] * inv[i], v[i][1] * inv[i], T());
+            if constexpr (INT8) {
+                reinterpret_cast<uint32_t*>(dst[i])[(D / 16) * g + md] = two;
+            } else {
+                reinterpret_cast<uint16_t*>(dst[i])[16 * md + g] = static_cast<uint16_t>(two);
+                reinterpret_cast<uint16_t*>(dst[i])[16 * md + g + 8] = static_cast<uint16_t>(two >> 16);
+            }
+        }
+    }
+
+private:
+    int64_t head;
+};
 
 // ---------------------------------------------------------------------------------------------------- the step
 template <class T, int D, bool INT8, int NB>
@@ -285,7 +304,8 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     extern __shared__ uint8_t smem[];
     __shared__ __align__(8) uint64_t full_bar[W][kStages];
     __shared__ uint32_t hole_s[W][kStages];                          // bit 4 i: the 16 keys i of the chunk lie in a hole
-    __shared__ float m_s[W][8 * NB], z_s[W][8 * NB], v_ref_s[W];
+    __shared__ __align__(8) float m_s[W][8 * NB], z_s[W][8 * NB];
+    __shared__ float v_ref_s[W];
     __shared__ int held_s[W];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     uint8_t* ring = smem + ((1024u - (ptx::smem_u32(smem) & 1023u)) & 1023u);      // (the swizzle's pattern repeats every 1 KB)
@@ -516,198 +536,216 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
             if (!failed && !landed(stage, phase)) failed = true;
             if (failed) break;
             any = true;
-            const uint32_t kst = ring_u32 + stage * kStageBytes, vst = kst + C::kVOff;
-            const uint8_t* const st = stages + stage * kStageBytes;
-            const int live = min(chunk, cc.len - start), blocks = (live + 15) >> 4;        // keys of the chunk
+            const int live = min(chunk, cc.len - start);      // keys of the chunk
             const uint32_t holes = hole_s[warp][stage];
-            const bool partial = live < CH || holes != 0u;
-            // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same)
-            float sc[MB][NB][4], v_mul[MB][2];
+            // `first_mb`: block of 16 keys; BLOCKS of them together, PART: keys of it may not exist
+            auto attend = [&](auto blocks, auto part, int first_mb) {
+                constexpr int BLOCKS = decltype(blocks)::value;
+                constexpr bool PART = decltype(part)::value;
+                const uint32_t kst = ring_u32 + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128)), vst = kst + C::kVOff;
+                const uint8_t* const st = stages + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128));
+                // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same).  Two sums, of the even and the odd
+                // steps: the chain of MMAs that wait for one another is half as long.
+                float sc[BLOCKS][NB][4], v_mul[BLOCKS][2];
+                float odd[BLOCKS][NB][4];
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) sc[mb][nb][0] = sc[mb][nb][1] = sc[mb][nb][2] = sc[mb][nb][3] = 0.f;
-                if (MB > 1 && mb >= blocks) continue;
-                if constexpr (INT8) {
-#pragma unroll
-                    for (int j = 0; j < D / 64; ++j) {
-                        const uint8_t* const at = st + (k_at ^ (64 * j)) + 16 * mb * D;
-                        const uint4 xa = *reinterpret_cast<const uint4*>(at), xb = *reinterpret_cast<const uint4*>(at + 8 * D);
-                        const uint32_t wa[4] = {xa.x, xa.y, xa.z, xa.w}, wb[4] = {xb.x, xb.y, xb.z, xb.w};
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const uint32_t ua = wa[w] ^ 0x80808080u, ub = wb[w] ^ 0x80808080u;
-                            const uint32_t a0 = codes_to_half2<false>(ua), a2 = codes_to_half2<true>(ua);
-                            const uint32_t a1 = codes_to_half2<false>(ub), a3 = codes_to_half2<true>(ub);
-#pragma unroll
-                            for (int nb = 0; nb < NB; ++nb)
-                                mma_16816<false>(sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
-                        }
-                    }
-                    const float* sk = scale_ring + stage * (CH * 2) + 16 * mb + k_row;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float dk = sk[8 * i];
-                        v_mul[mb][i] = sk[CH + 8 * i];
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) { sc[mb][nb][2 * i] *= dk; sc[mb][nb][2 * i + 1] *= dk; }
-                    }
-                } else {
-                    const int row = 16 * mb + (lane & 15), piece = lane >> 4;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        uint32_t a[4];
-                        ldmatrix_x4<false>(a, kst + value_piece<CH>(row, 2 * i + piece));
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
-                    }
-                }
-            }
-            // ---- keys past the end and in holes do not exist, whatever lies in their rows
-            if (partial) {
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    const bool hole = (holes >> (4 * mb)) & 1u;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int key = 16 * mb + 8 * i + (INT8 ? key_of_row<D>(g) : g);
-                        if (key < live && !hole) continue;
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) sc[mb][nb][2 * i] = sc[mb][nb][2 * i + 1] = -INFINITY;
-                        v_mul[mb][i] = 0.f;
-                    }
-                }
-                if constexpr (!INT8) {
-                    // (0 times a NaN is one)
-                    for (int i = lane; i < (CH - live) * (D / 8); i += 32) {
-                        const int row = live + i / (D / 8), piece = i & (D / 8 - 1);
-                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vst + value_piece<CH>(row, piece)), "r"(0u) : "memory");
-                    }
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                }
-            }
-            // ---- exponents, relative to the running maximum; it moves when one of them passes the line
-            float top = -INFINITY;
-            auto exponents = [&](float (&e)[MB][NB][4]) {
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
+                for (int mb = 0; mb < BLOCKS; ++mb)
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]);
-            };
-            float e[MB][NB][4];
-            exponents(e);
+                        for (int k = 0; k < 4; ++k) sc[mb][nb][k] = odd[mb][nb][k] = 0.f;
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
+                for (int mb = 0; mb < BLOCKS; ++mb) {
+                    if constexpr (INT8) {
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) top = fmax3(fmax3(top, e[mb][nb][0], e[mb][nb][1]), e[mb][nb][2], e[mb][nb][3]);
-            bool past = top > C::kOff + C::kLine;
-            if constexpr (INT8) {
-                float v_top = fmaxf(v_mul[0][0], v_mul[0][1]);
+                        for (int j = 0; j < D / 64; ++j) {
+                            const uint8_t* const at = st + (k_at ^ (64 * j)) + 16 * mb * D;
+                            const uint4 xa = *reinterpret_cast<const uint4*>(at), xb = *reinterpret_cast<const uint4*>(at + 8 * D);
+                            const uint32_t wa[4] = {xa.x, xa.y, xa.z, xa.w}, wb[4] = {xb.x, xb.y, xb.z, xb.w};
 #pragma unroll
-                for (int mb = 1; mb < MB; ++mb) v_top = fmax3(v_top, v_mul[mb][0], v_mul[mb][1]);
-                past = past || v_top > v_ref;
-            }
-            if (__any_sync(0xffffffffu, past)) {
-                float alpha[NB][2];
+                            for (int w = 0; w < 4; ++w) {
+                                const uint32_t ua = wa[w] ^ 0x80808080u, ub = wb[w] ^ 0x80808080u;
+                                const uint32_t a0 = codes_to_half2<false>(ua), a2 = codes_to_half2<true>(ua);
+                                const uint32_t a1 = codes_to_half2<false>(ub), a3 = codes_to_half2<true>(ub);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
+                                for (int nb = 0; nb < NB; ++nb)
+                                    mma_16816<false>(w & 1 ? odd[mb][nb] : sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
+                            }
+                        }
+                    } else {
+                        const int row = 16 * mb + (lane & 15), piece = lane >> 4;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        float x = fmaxf(sc[0][nb][k], sc[0][nb][2 + k]);
+                        for (int i = 0; i < D / 16; ++i) {
+                            uint32_t a[4];
+                            ldmatrix_x4<false>(a, kst + value_piece<CH>(row, 2 * i + piece));
 #pragma unroll
-                        for (int mb = 1; mb < MB; ++mb) x = fmax3(x, sc[mb][nb][k], sc[mb][nb][2 + k]);
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                        const float s_new = fminf(sub[nb][k], C::kOff - ceilf(x * q_mul[nb][k]));
-                        alpha[nb][k] = exp2f(s_new - sub[nb][k]);
-                        sub[nb][k] = s_new;
-                        z[nb][k] *= alpha[nb][k];
-                    }
-                if constexpr (INT8) {
-                    uint32_t dv = 0u;
-#pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) dv = max(dv, max(__float_as_uint(fabsf(v_mul[mb][0])), __float_as_uint(fabsf(v_mul[mb][1]))));
-                    dv = __reduce_max_sync(0xffffffffu, dv);
-                    const uint32_t want = (min(dv, 0x7e800000u) + 0x7fffffu) & 0x7f800000u, have = __float_as_uint(v_ref);
-                    if (want > have) {          // (the same in the whole warp)
-                        const float back = __uint_as_float(have) * __uint_as_float(0x7f000000u - want);
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) { alpha[nb][0] *= back; alpha[nb][1] *= back; }
-                        v_ref = __uint_as_float(want);
+                            for (int nb = 0; nb < NB; ++nb)
+                                mma_16816<BF16>(i & 1 ? odd[mb][nb] : sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
+                        }
                     }
                 }
+                const float* const sk = scale_ring + stage * (CH * 2) + 16 * first_mb + k_row;
 #pragma unroll
-                for (int md = 0; md < D / 16; ++md)
+                for (int mb = 0; mb < BLOCKS; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float dk = 1.f;
+                        if constexpr (INT8) { dk = sk[16 * mb + 8 * i]; v_mul[mb][i] = sk[CH + 16 * mb + 8 * i]; }
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                sc[mb][nb][2 * i + k] += odd[mb][nb][2 * i + k];
+                                if constexpr (INT8) sc[mb][nb][2 * i + k] *= dk;
+                            }
+                    }
+                // ---- keys past the end and in holes do not exist, whatever lies in their rows
+                if constexpr (PART) {
+                    const bool hole = (holes >> (4 * first_mb)) & 1u;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (16 * first_mb + 8 * i + (INT8 ? k_row : g) < live && !hole) continue;
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) sc[0][nb][2 * i] = sc[0][nb][2 * i + 1] = -INFINITY;
+                        v_mul[0][i] = 0.f;
+                    }
+                    if constexpr (!INT8) {
+                        const int left = live - 16 * first_mb;          // (0 times a NaN is one)
+                        if (left < 16) {
+                            for (int i = lane; i < (16 - left) * (D / 8); i += 32) {
+                                const int row = left + i / (D / 8), piece = i & (D / 8 - 1);
+                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vst + value_piece<CH>(row, piece)), "r"(0u) : "memory");
+                            }
+                            ptx::fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                    }
+                }
+                // ---- exponents, relative to the running maximum; it moves when one of them passes the line
+                float top = -INFINITY;
+                float e[BLOCKS][NB][4];
+                auto exponents = [&]() {
+#pragma unroll
+                    for (int mb = 0; mb < BLOCKS; ++mb)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]);
+                };
+                exponents();
+#pragma unroll
+                for (int mb = 0; mb < BLOCKS; ++mb)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) top = fmax3(fmax3(top, e[mb][nb][0], e[mb][nb][1]), e[mb][nb][2], e[mb][nb][3]);
+                bool past = top > C::kOff + C::kLine;
+                if constexpr (INT8) {
+                    float v_top = fmaxf(v_mul[0][0], v_mul[0][1]);
+#pragma unroll
+                    for (int mb = 1; mb < BLOCKS; ++mb) v_top = fmax3(v_top, v_mul[mb][0], v_mul[mb][1]);
+                    past = past || v_top > v_ref;
+                }
+                if (__any_sync(0xffffffffu, past)) {
+                    float alpha[NB][2];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            float x = fmaxf(sc[0][nb][k], sc[0][nb][2 + k]);
+#pragma unroll
+                            for (int mb = 1; mb < BLOCKS; ++mb) x = fmax3(x, sc[mb][nb][k], sc[mb][nb][2 + k]);
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            const float s_new = fminf(sub[nb][k], C::kOff - ceilf(x * q_mul[nb][k]));
+                            alpha[nb][k] = fast_exp2(s_new - sub[nb][k]);
+                            sub[nb][k] = s_new;
+                            z[nb][k] *= alpha[nb][k];
+                        }
+                    if constexpr (INT8) {
+                        uint32_t dv = 0u;
+#pragma unroll
+                        for (int mb = 0; mb < BLOCKS; ++mb) dv = max(dv, max(__float_as_uint(fabsf(v_mul[mb][0])), __float_as_uint(fabsf(v_mul[mb][1]))));
+                        dv = __reduce_max_sync(0xffffffffu, dv);
+                        const uint32_t want = (min(dv, 0x7e800000u) + 0x7fffffu) & 0x7f800000u, have = __float_as_uint(v_ref);
+                        if (want > have) {          // (the same in the whole warp)
+                            const float back = __uint_as_float(have) * __uint_as_float(0x7f000000u - want);
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) { alpha[nb][0] *= back; alpha[nb][1] *= back; }
+                            v_ref = __uint_as_float(want);
+                        }
+                    }
+#pragma unroll
+                    for (int md = 0; md < D / 16; ++md)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            acc[md][nb][0] *= alpha[nb][0]; acc[md][nb][1] *= alpha[nb][1];
+                            acc[md][nb][2] *= alpha[nb][0]; acc[md][nb][3] *= alpha[nb][1];
+                        }
+                    exponents();
+                }
+                const float inv = __uint_as_float(0x7f000000u - __float_as_uint(v_ref));
+                // ---- probabilities, and O^T += V^T P^T block by block
+#pragma unroll
+                for (int mb = 0; mb < BLOCKS; ++mb) {
+                    uint32_t p0[NB], p1[NB];
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
-                        acc[md][nb][0] *= alpha[nb][0]; acc[md][nb][1] *= alpha[nb][1];
-                        acc[md][nb][2] *= alpha[nb][0]; acc[md][nb][3] *= alpha[nb][1];
+                        float p[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            p[k] = fast_exp2(e[mb][nb][k]);
+                            z[nb][k & 1] += p[k];
+                            if constexpr (INT8) p[k] *= v_mul[mb][k >> 1] * inv;
+                        }
+                        using P = typename std::conditional<C::kHalfP, __half, __nv_bfloat16>::type;
+                        p0[nb] = transpose_8x8(act_pack2(p[0], p[1], P()));
+                        p1[nb] = transpose_8x8(act_pack2(p[2], p[3], P()));
                     }
-                exponents(e);
-            }
-            const float inv = __uint_as_float(0x7f000000u - __float_as_uint(v_ref));
-            // ---- probabilities, and O^T += V^T P^T block by block
+                    if constexpr (INT8) {
+                        // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
+                        uint32_t x[4][D / 32];
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                if (MB > 1 && mb >= blocks) continue;
-                uint32_t p0[NB], p1[NB];
+                        for (int i = 0; i < 4; ++i) {
+                            const uint8_t* const at = st + (i & 1 ? v_at1 : v_at0) + (16 * mb + 8 * (i >> 1)) * D;
+                            if constexpr (D == 128) {
+                                const uint4 v = *reinterpret_cast<const uint4*>(at);
+                                x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+                            } else {
+                                const uint2 v = *reinterpret_cast<const uint2*>(at);
+                                x[i][0] = v.x; x[i][1] = v.y;
+                            }
+                        }
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    float p[4];
+                        for (int w = 0; w < D / 32; ++w) {
+                            const uint32_t u0 = x[0][w] ^ 0x80808080u, u1 = x[1][w] ^ 0x80808080u;
+                            const uint32_t u2 = x[2][w] ^ 0x80808080u, u3 = x[3][w] ^ 0x80808080u;
+                            const uint32_t lo01 = __byte_perm(u0, u1, 0x5140), hi01 = __byte_perm(u0, u1, 0x7362);
+                            const uint32_t lo23 = __byte_perm(u2, u3, 0x5140), hi23 = __byte_perm(u2, u3, 0x7362);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        p[k] = fast_exp2(e[mb][nb][k]);
-                        z[nb][k & 1] += p[k];
-                        if constexpr (INT8) p[k] *= v_mul[mb][k >> 1] * inv;
-                    }
-                    using P = typename std::conditional<C::kHalfP, __half, __nv_bfloat16>::type;
-                    p0[nb] = transpose_8x8(act_pack2(p[0], p[1], P()));
-                    p1[nb] = transpose_8x8(act_pack2(p[2], p[3], P()));
-                }
-                if constexpr (INT8) {
-                    // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
-                    uint32_t x[4][D / 32];
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t a01 = h ? hi01 : lo01, a23 = h ? hi23 : lo23;
+                                const uint32_t a0 = codes_to_half2<false>(a01), a1 = codes_to_half2<true>(a01);
+                                const uint32_t a2 = codes_to_half2<false>(a23), a3 = codes_to_half2<true>(a23);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint8_t* const at = st + (i & 1 ? v_at1 : v_at0) + (16 * mb + 8 * (i >> 1)) * D;
-                        if constexpr (D == 128) {
-                            const uint4 v = *reinterpret_cast<const uint4*>(at);
-                            x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
-                        } else {
-                            const uint2 v = *reinterpret_cast<const uint2*>(at);
-                            x[i][0] = v.x; x[i][1] = v.y;
+                                for (int nb = 0; nb < NB; ++nb) mma_16816<false>(acc[2 * w + h][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
+                            }
+                        }
+                    } else {
+                        const int row = 16 * mb + (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1;
+#pragma unroll
+                        for (int md = 0; md < D / 16; ++md) {
+                            uint32_t a[4];
+                            ldmatrix_x4<true>(a, vst + value_piece<CH>(row, 2 * md + piece));
+#pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
                         }
                     }
-#pragma unroll
-                    for (int w = 0; w < D / 32; ++w) {
-                        const uint32_t u0 = x[0][w] ^ 0x80808080u, u1 = x[1][w] ^ 0x80808080u;
-                        const uint32_t u2 = x[2][w] ^ 0x80808080u, u3 = x[3][w] ^ 0x80808080u;
-                        const uint32_t lo01 = __byte_perm(u0, u1, 0x5140), hi01 = __byte_perm(u0, u1, 0x7362);
-                        const uint32_t lo23 = __byte_perm(u2, u3, 0x5140), hi23 = __byte_perm(u2, u3, 0x7362);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t a01 = h ? hi01 : lo01, a23 = h ? hi23 : lo23;
-                            const uint32_t a0 = codes_to_half2<false>(a01), a1 = codes_to_half2<true>(a01);
-                            const uint32_t a2 = codes_to_half2<false>(a23), a3 = codes_to_half2<true>(a23);
-#pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) mma_16816<false>(acc[2 * w + h][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
-                        }
-                    }
-                } else {
-                    const int row = 16 * mb + (lane & 7) + 8 * (lane >> 4), piece = (lane >> 3) & 1;
-#pragma unroll
-                    for (int md = 0; md < D / 16; ++md) {
-                        uint32_t a[4];
-                        ldmatrix_x4<true>(a, vst + value_piece<CH>(row, 2 * md + piece));
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
-                    }
                 }
-            }
+            };
+            if (live == CH && holes == 0u) attend(std::integral_constant<int, MB>(), std::false_type(), 0);
+            else
+#pragma unroll 1
+                for (int mb = 0; 16 * mb < live; ++mb) attend(std::integral_constant<int, 1>(), std::true_type(), mb);
             held = stage;
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
             ++taken;
@@ -746,25 +784,52 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 for (int md = 0; md < D / 16; ++md)
                     mine[md * 32 + lane] = make_float4(acc[md][nb][0], acc[md][nb][1], acc[md][nb][2], acc[md][nb][3]);
             team_sync();
-            const int w0 = warp - member, n = 8 * nb + 2 * t;
-            float m[2] = {m_s[w0][n], m_s[w0][n + 1]};
-            for (int w = w0 + 1; w < w0 + team; ++w) { m[0] = fmaxf(m[0], m_s[w][n]); m[1] = fmaxf(m[1], m_s[w][n + 1]); }
-#pragma unroll 1
-            for (int md = member; md < D / 16; md += team) {
-                float zz[2] = {0.f, 0.f};
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                for (int w = w0; w < w0 + team; ++w) {
-                    const float f0 = exp2f(m_s[w][n] - m[0]) * C::kUnOff, f1 = exp2f(m_s[w][n + 1] - m[1]) * C::kUnOff, ref = v_ref_s[w];
-                    zz[0] += z_s[w][n] * f0; zz[1] += z_s[w][n + 1] * f1;
-                    if (ref < 0.f) continue;
-                    const float4 x = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes)[md * 32 + lane];
-                    o.x += x.x * (f0 * ref); o.y += x.y * (f1 * ref); o.z += x.z * (f0 * ref); o.w += x.w * (f1 * ref);
+            // (all loads first: what this costs is latency)
+            const int n = 8 * nb + 2 * t;
+            float2 mw[W], zw[W];
+            float refs[W], m[2] = {kNoMax, kNoMax}, zz[2] = {0.f, 0.f};
+            const float4* frags[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                mw[w] = *reinterpret_cast<const float2*>(&m_s[w][n]);
+                zw[w] = *reinterpret_cast<const float2*>(&z_s[w][n]);
+                refs[w] = (w >> work.team_shift) == team_no ? v_ref_s[w] : -1.f;
+                if ((w >> work.team_shift) != team_no) { mw[w] = make_float2(kNoMax, kNoMax); zw[w] = make_float2(0.f, 0.f); }
+                frags[w] = reinterpret_cast<const float4*>(ring + (w * kStages + held_s[w]) * kStageBytes) + lane;
+                m[0] = fmaxf(m[0], mw[w].x); m[1] = fmaxf(m[1], mw[w].y);
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) {                     // (the maxima are whole numbers)
+                mw[w] = make_float2(fast_exp2(mw[w].x - m[0]) * C::kUnOff, fast_exp2(mw[w].y - m[1]) * C::kUnOff);
+                zz[0] += zw[w].x * mw[w].x; zz[1] += zw[w].y * mw[w].y;
+                mw[w].x *= refs[w]; mw[w].y *= refs[w];
+            }
+            constexpr int kMost = D / 16 / C::kMinTeam;
+            float4 o[kMost];
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const int md = member + i * team;
+                o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (md >= D / 16) continue;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    if (refs[w] < 0.f) continue;
+                    const float4 x = frags[w][md * 32];
+                    o[i].x += x.x * mw[w].x; o[i].y += x.y * mw[w].y; o[i].z += x.z * mw[w].x; o[i].w += x.w * mw[w].y;
                 }
-                if (whole) write_out<T, D, INT8, NB>(prm, b, h, md, nb, lane, o, m, zz);
-                else prm.part_o[(static_cast<int64_t>(slot) * NB + nb) * C::kFrag + md * 32 + lane] = o;
-                if (!whole && md == 0 && g == 0)
-                    *reinterpret_cast<float4*>(prm.part_mz + slot * (8 * NB) + n) = make_float4(m[0], zz[0], m[1], zz[1]);
+            }
+            if (whole) {
+                OutRows<T, D, INT8> rows(prm, b, h, 8 * NB, nb, lane);
+                rows.sums(prm, m, zz, member == 0 && g == 0);
+#pragma unroll
+                for (int i = 0; i < kMost; ++i)
+                    if (member + i * team < D / 16) rows.store(member + i * team, lane, o[i]);
+            } else {
+                float4* part = prm.part_o + (static_cast<int64_t>(slot) * NB + nb) * C::kFrag + lane;
+#pragma unroll
+                for (int i = 0; i < kMost; ++i)
+                    if (member + i * team < D / 16) part[(member + i * team) * 32] = o[i];
+                if (member == 0 && g == 0) *reinterpret_cast<float4*>(prm.part_mz + slot * (8 * NB) + n) = make_float4(m[0], zz[0], m[1], zz[1]);
             }
             if (nb == NB - 1) ptx::fence_proxy_async_smem();  // the stages go back to the copies
             team_sync();
@@ -783,80 +848,83 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 }
 
 // Joins the parts of the rows that several workers shared.  A job (row, s, w, n) names slot s and the first slots of n workers
-// from w on.  What bounds it is the round trips: the parts are loaded eight at a time.  A row of up to eight parts has a warp
-// for every fragment; the parts of others are shared out over the warps, fragment by fragment (by a block each where rows are few).
-constexpr int kJoinWarps = 8, kJoinAtOnce = 8;
-template <class T, int D, bool INT8, int NB>
-__global__ void __launch_bounds__(32 * kJoinWarps)
+// from w on.  What bounds it is the round trips: the parts are loaded kJoinAtOnce at a time.  A row of up to that many has a
+// warp for every fragment; the parts of others are shared out over the warps, fragment by fragment (by a block each where rows
+// are few).
+constexpr int kJoinAtOnce = 8;
+struct Part {
+    float4 o, mz;                   // sums; maximum and sum of column 2 t, of column 2 t + 1
+};
+// (maxima are whole numbers, so the weights are exact)
+template <int N>
+__device__ __forceinline__ Part join_parts(const Part (&p)[N]) {
+    Part r;
+    r.mz = make_float4(kNoMax, 0.f, kNoMax, 0.f);
+    r.o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) { r.mz.x = fmaxf(r.mz.x, p[i].mz.x); r.mz.z = fmaxf(r.mz.z, p[i].mz.z); }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float f0 = fast_exp2(p[i].mz.x - r.mz.x), f1 = fast_exp2(p[i].mz.z - r.mz.z);
+        r.mz.y += p[i].mz.y * f0; r.mz.w += p[i].mz.w * f1;
+        r.o.x += p[i].o.x * f0; r.o.y += p[i].o.y * f1; r.o.z += p[i].o.z * f0; r.o.w += p[i].o.w * f1;
+    }
+    return r;
+}
+template <class T, int D, bool INT8, int NB, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
 paged_join_kernel(const PagedDecodeParams prm) {
     using C = Cfg<T, D, INT8, NB>;
-    __shared__ float4 o_s[kJoinWarps][32];
-    __shared__ float4 mz_s[kJoinWarps][32];
+    __shared__ Part part_s[WARPS][32];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
     const int4 job = __ldcg(prm.join + blockIdx.x);
     if (job.x < 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, parts = job.w + 1;
-    const int b = job.x / prm.HG, h = job.x - b * prm.HG;
     constexpr int F = (D / 16) * NB;
     const int f_begin = blockIdx.y * F / gridDim.y, f_end = (blockIdx.y + 1) * F / gridDim.y;
-
-    float4 o;
-    float m[2], z[2];
-    auto clear = [&]() {
-        o = make_float4(0.f, 0.f, 0.f, 0.f);
-        m[0] = m[1] = kNoMax;
-        z[0] = z[1] = 0.f;
-    };
-    auto add = [&](const float4& x, const float4& mz) {
-        float back[2], fore[2];
-        const float mm[2] = {mz.x, mz.z}, zz[2] = {mz.y, mz.w};
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float top = fmaxf(m[k], mm[k]);
-            back[k] = exp2f(m[k] - top);
-            fore[k] = exp2f(mm[k] - top);
-            z[k] = z[k] * back[k] + zz[k] * fore[k];
-            m[k] = top;
-        }
-        o.x = o.x * back[0] + x.x * fore[0]; o.y = o.y * back[1] + x.y * fore[1];
-        o.z = o.z * back[0] + x.z * fore[0]; o.w = o.w * back[1] + x.w * fore[1];
-    };
     // parts first, first + step, ... of fragment f = nb D / 16 + md
-    auto add_parts = [&](int f, int first, int step) {
+    auto take = [&](int f, int first, int step) -> Part {
         const int nb = f / (D / 16);
-        for (int i0 = first; i0 < parts; i0 += step * kJoinAtOnce) {
-            float4 x[kJoinAtOnce], mz[kJoinAtOnce];
+        Part sum;
+        for (int i0 = first;; i0 += step * kJoinAtOnce) {
+            Part p[kJoinAtOnce + 1];
 #pragma unroll
             for (int j = 0; j < kJoinAtOnce; ++j) {
                 const int i = i0 + j * step;
+                p[j].mz = make_float4(kNoMax, 0.f, kNoMax, 0.f);
+                p[j].o = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (i >= parts) continue;
                 const int64_t slot = i == 0 ? job.y : 2 * (job.z + i - 1);
-                x[j] = __ldcg(prm.part_o + slot * (NB * C::kFrag) + f * 32 + lane);
-                mz[j] = __ldcg(reinterpret_cast<const float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t));
+                p[j].o = __ldcg(prm.part_o + slot * (NB * C::kFrag) + f * 32 + lane);
+                p[j].mz = __ldcg(reinterpret_cast<const float4*>(prm.part_mz + slot * (8 * NB) + 8 * nb + 2 * t));
             }
-#pragma unroll
-            for (int j = 0; j < kJoinAtOnce; ++j)
-                if (i0 + j * step < parts) add(x[j], mz[j]);
+            if (i0 == first) { p[kJoinAtOnce].o = make_float4(0.f, 0.f, 0.f, 0.f); p[kJoinAtOnce].mz = make_float4(kNoMax, 0.f, kNoMax, 0.f); }
+            else p[kJoinAtOnce] = sum;
+            sum = join_parts(p);
+            if (i0 + step * kJoinAtOnce >= parts) return sum;
         }
     };
+    const int b = job.x / prm.HG, h = job.x - b * prm.HG;
+    auto finish = [&](int f, const Part& p) {
+        const int nb = f / (D / 16), md = f % (D / 16);
+        OutRows<T, D, INT8> rows(prm, b, h, 8 * NB, nb, lane);
+        const float m[2] = {p.mz.x, p.mz.z}, z[2] = {p.mz.y, p.mz.w};
+        rows.sums(prm, m, z, md == 0 && lane < 4);
+        rows.store(md, lane, p.o);
+    };
     if (parts <= kJoinAtOnce) {
-        for (int f = f_begin + warp; f < f_end; f += kJoinWarps) {
-            clear();
-            add_parts(f, 0, 1);
-            write_out<T, D, INT8, NB>(prm, b, h, f % (D / 16), f / (D / 16), lane, o, m, z);
-        }
+        for (int f = f_begin + warp; f < f_end; f += WARPS) finish(f, take(f, 0, 1));
         return;
     }
     for (int f = f_begin; f < f_end; ++f) {
-        clear();
-        add_parts(f, warp, kJoinWarps);
-        o_s[warp][lane] = o;
-        mz_s[warp][lane] = make_float4(m[0], z[0], m[1], z[1]);
+        part_s[warp][lane] = take(f, warp, WARPS);
         __syncthreads();
         if (warp == 0) {
-            for (int w = 1; w < kJoinWarps; ++w) add(o_s[w][lane], mz_s[w][lane]);
-            write_out<T, D, INT8, NB>(prm, b, h, f % (D / 16), f / (D / 16), lane, o, m, z);
+            Part p[WARPS];
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) p[w] = part_s[w][lane];
+            finish(f, join_parts(p));
         }
         __syncthreads();
     }
@@ -950,9 +1018,11 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     e = cudaLaunchKernelEx(&cfg, kernel, prm, maps);
     g_launch_count.fetch_add(1);
     if (e != cudaSuccess || !plan.splits) return static_cast<int>(e);
-    const int F = (D / 16) * NB;
-    cfg.gridDim = dim3(plan.jobs, prm.jobs_by_row && plan.jobs < plan.ctas ? F : 1); cfg.blockDim = dim3(32 * kJoinWarps); cfg.dynamicSmemBytes = 0;
-    e = cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB>, prm);
+    // few rows: many parts each, a block a fragment; many rows: few parts
+    const bool few = prm.jobs_by_row && plan.jobs < plan.ctas;
+    constexpr int kFew = 16, kMany = 4;
+    cfg.gridDim = dim3(plan.jobs, few ? (D / 16) * NB : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
+    e = few ? cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kFew>, prm) : cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kMany>, prm);
     g_launch_count.fetch_add(1);
     return static_cast<int>(e);
 }
