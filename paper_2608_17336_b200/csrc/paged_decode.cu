@@ -1018,10 +1018,11 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     e = cudaLaunchKernelEx(&cfg, kernel, prm, maps);
     g_launch_count.fetch_add(1);
     if (e != cudaSuccess || !plan.splits) return static_cast<int>(e);
-    // few rows: many parts each, a block a fragment; many rows: few parts
-    const bool few = prm.jobs_by_row && plan.jobs < plan.ctas;
-    constexpr int kFew = 16, kMany = 4;
-    cfg.gridDim = dim3(plan.jobs, few ? (D / 16) * NB : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
+    // few rows: many parts each, a block of sixteen warps for a fragment; otherwise the parts of a row go at once, to the
+    // warps of one block (64 rows of seven parts: 1.5 us so, 7 in large blocks, which an SM holds one of)
+    const bool few = prm.jobs_by_row && static_cast<int64_t>(plan.jobs) * kJoinAtOnce < plan.ctas;
+    constexpr int kFew = 16, kMany = 4, F = (D / 16) * NB;
+    cfg.gridDim = dim3(plan.jobs, few ? F : plan.jobs <= kSms ? F / kMany : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
     e = few ? cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kFew>, prm) : cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kMany>, prm);
     g_launch_count.fetch_add(1);
     return static_cast<int>(e);
