@@ -1,10 +1,12 @@
 // Paged key/value cache: the checks of its description, writing new tokens (quantised where the cache is INT8) and reading
-// contexts back.  Both kernels move bytes: a row of head_dim values of one (token, head) is taken by d / 8 lanes, 16 bytes of
-// the 16-bit side each, K and V together.
+// contexts back.  Both kernels move bytes: a row of head_dim values of one (token, head) is taken by d / 16 lanes, K and V
+// together.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "paged.cuh"
+#include "ptx_sm100.cuh"
 #include "quant8.cuh"
 
 namespace tilemix {
@@ -72,7 +74,11 @@ int resolve_paged(const tilemix_paged_t* p, PagedCache* c) {
 
 namespace {
 
-constexpr int kMoveThreads = 256;
+// A lane takes kPieces pieces of eight values, 16 bytes of the 16-bit side, of one row; neighbouring lanes neighbouring pieces,
+// so that every access of a warp is whole sectors.  One, two and four of them: read-back of 24 K tokens, 8 heads of 128, INT8
+// 33.2 / 27.3 / 27.2 us, of 16 ragged BF16 contexts, heads of 64 79.9 / 72.3 / 76.5, 64 new tokens appended and read back
+// 5.1 / 5.6 / 6.6; two rows of two pieces 28.4 / 72.6 / 7.8.  Blocks of 512 threads: 28.4, 72.3, 6.4.
+constexpr int kMoveThreads = 128, kPieces = 2;
 
 struct MoveParams {
     PagedCache c;
@@ -99,72 +105,91 @@ __device__ __forceinline__ int owner_of(const int32_t* __restrict__ cu, int B, i
     return n;
 }
 
-// The quantiser of one row, in the d / 8 lanes that hold it: codes of this lane's eight values, and the scale.
+// The quantiser of one row, in the lanes that hold it: codes of this lane's values, and the scale.
 // delta = RN(max|x| / 127), x8 = RN_int(RN(x / delta)).  The maximum is taken over the bit patterns, which order like the
 // magnitudes and put infinities and NaN on top.  quant_scale's one-FMA form of the rounded quotient was derived for binary16;
 // it holds for bfloat16 too: its ratios of 8-bit integers stay further from the half-integers than those of 11-bit ones, and
 // the exact half-integers are the same two kinds.  It needs delta and 1 / delta to be normal numbers, hence the division for
 // rows whose maximum is below 2^-100 (bfloat16 only).
-template <class T, int LANES>
-__device__ __forceinline__ uint2 quantise_row(const uint4& x, float* delta) {
-    constexpr bool BF16 = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+__device__ __forceinline__ uint2 quant8_bf16(const uint4& x, const QuantScale& s, bool divide) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t m2 = __vmaxu2(__vmaxu2(habs2_bits(w[0]), habs2_bits(w[1])), __vmaxu2(habs2_bits(w[2]), habs2_bits(w[3])));
+    uint32_t code[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = act_to_float2(w[i], __nv_bfloat16());
+        if (divide) {
+            code[2 * i] = max(-127, min(127, __float2int_rn(__fdiv_rn(f.x, s.delta))));
+            code[2 * i + 1] = max(-127, min(127, __float2int_rn(__fdiv_rn(f.y, s.delta))));
+        } else {
+            const float2 r2 = make_float2(s.r, s.r), magic = make_float2(12582912.f, 12582912.f);
+            float2 y = __ffma2_rn(f, r2, magic);
+            if (s.refine) {
+                const float2 q = __fmul2_rn(f, r2);
+                y = __fadd2_rn(__ffma2_rn(__ffma2_rn(make_float2(-s.delta, -s.delta), q, f), r2, q), magic);
+            }
+            code[2 * i] = __float_as_uint(y.x); code[2 * i + 1] = __float_as_uint(y.y);
+        }
+    }
+    const uint32_t p0 = __byte_perm(code[0], code[1], 0x0040), p1 = __byte_perm(code[2], code[3], 0x0040);
+    const uint32_t p2 = __byte_perm(code[4], code[5], 0x0040), p3 = __byte_perm(code[6], code[7], 0x0040);
+    return make_uint2(__byte_perm(p0, p1, 0x5410), __byte_perm(p2, p3, 0x5410));
+}
+template <class T, int LANES, int P>
+__device__ __forceinline__ float quantise_row(const uint4 (&x)[P], uint2 (&code)[P]) {
+    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+    uint32_t m2 = 0u;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        m2 = __vmaxu2(m2, __vmaxu2(__vmaxu2(habs2_bits(x[i].x), habs2_bits(x[i].y)), __vmaxu2(habs2_bits(x[i].z), habs2_bits(x[i].w))));
     uint32_t m = max(m2 & 0xffffu, m2 >> 16);
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (m >= (BF16 ? 0x7f80u : 0x7c00u)) {
-        *delta = __int_as_float(0x7fc00000);
-        return make_uint2(0u, 0u);
+    const bool odd = m >= (BF16 ? 0x7f80u : 0x7c00u);
+    if (odd || m == 0u) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) code[i] = make_uint2(0u, 0u);
+        return odd ? __int_as_float(0x7fc00000) : 0.f;
     }
     const float amax = BF16 ? __uint_as_float(m << 16) : __half2float(__ushort_as_half(static_cast<unsigned short>(m)));
-    if (amax == 0.f) {
-        *delta = 0.f;
-        return make_uint2(0u, 0u);
-    }
-    if constexpr (!BF16) {
-        const QuantScale s = quant_scale(amax);
-        *delta = s.delta;
-        return quant8(x, s);
-    } else {
-        int code[8];
-        if (amax < 7.888609052210118e-31f) {
-            *delta = __fdiv_rn(amax, 127.f);
+    const bool tiny = BF16 && amax < 7.888609052210118e-31f;
+    QuantScale s;
+    if (tiny) { s.delta = __fdiv_rn(amax, 127.f); s.r = 0.f; s.refine = false; }
+    else s = quant_scale(amax);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = act_to_float2(w[i], T());
-                code[2 * i] = max(-127, min(127, __float2int_rn(__fdiv_rn(f.x, *delta))));
-                code[2 * i + 1] = max(-127, min(127, __float2int_rn(__fdiv_rn(f.y, *delta))));
-            }
-        } else {
-            const QuantScale s = quant_scale(amax);
-            *delta = s.delta;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 f2 = act_to_float2(w[i / 2], T());
-                const float f = i % 2 ? f2.y : f2.x;
-                float y = __fmaf_rn(f, s.r, 12582912.f);
-                if (s.refine) {
-                    const float q = __fmul_rn(f, s.r);
-                    y = __fadd_rn(__fmaf_rn(__fmaf_rn(-s.delta, q, f), s.r, q), 12582912.f);
-                }
-                code[i] = static_cast<int>(__float_as_uint(y));
-            }
-        }
-        const uint32_t p0 = __byte_perm(code[0], code[1], 0x0040), p1 = __byte_perm(code[2], code[3], 0x0040);
-        const uint32_t p2 = __byte_perm(code[4], code[5], 0x0040), p3 = __byte_perm(code[6], code[7], 0x0040);
-        return make_uint2(__byte_perm(p0, p1, 0x5410), __byte_perm(p2, p3, 0x5410));
+    for (int i = 0; i < P; ++i) {
+        if constexpr (BF16) code[i] = quant8_bf16(x[i], s, tiny);
+        else code[i] = quant8(x[i], s);
     }
+    return s.delta;
+}
+
+// The values that eight codes stand for: FP32 products, rounded.  A byte x + 128 under 0x4b0000 is the float 2^23 + x + 128.
+// (The conversion instruction has a quarter of the rate.)
+template <class T>
+__device__ __forceinline__ uint4 dequantise8(const uint2& code, float delta) {
+    const float2 off = make_float2(-8388736.f, -8388736.f), d2 = make_float2(delta, delta);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t biased = (i < 2 ? code.x : code.y) ^ 0x80808080u;
+        const float2 f = make_float2(__uint_as_float(__byte_perm(biased, 0x4b000000u, i & 1 ? 0x7652 : 0x7650)),
+                                     __uint_as_float(__byte_perm(biased, 0x4b000000u, i & 1 ? 0x7653 : 0x7651)));
+        const float2 v = __fmul2_rn(__fadd2_rn(f, off), d2);
+        w[i] = act_pack2(v.x, v.y, T());
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // New rows into the cache.  Row = (token, head), heads innermost, as the inputs lie.
 template <class T, int D, bool INT8>
 __global__ void __launch_bounds__(kMoveThreads)
 paged_append_kernel(const MoveParams prm) {
-    constexpr int LANES = D / 8, ROWS = kMoveThreads / LANES;
+    constexpr int P = kPieces, LANES = D / 8 / P, ROWS = kMoveThreads / LANES;
     const PagedCache& c = prm.c;
     const int row = blockIdx.x * ROWS + threadIdx.x / LANES, part = threadIdx.x % LANES;
     const int t = row / c.Hk, head = row - t * c.Hk;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     int b = t, n_new = 1, i = 0;
     if (prm.cu != nullptr) {
         // the sequence of the warp's first row; a warp's rows are few tokens, so the others are at most a step or two on
@@ -175,56 +200,54 @@ paged_append_kernel(const MoveParams prm) {
             n_new = prm.cu[b + 1] - prm.cu[b];
         }
     }
-    int page = -1, pos = 0;
+    int page = -1, at = 0;
+    uint4 k[P], v[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) k[p] = v[p] = make_uint4(0u, 0u, 0u, 0u);
     if (row < prm.rows && b < c.B && i >= 0) {
-        pos = paged_len(c, b) - n_new + i;
+        const uint4* kf = reinterpret_cast<const uint4*>(prm.k + t * prm.k_st[2] + head * prm.k_st[1]) + part;
+        const uint4* vf = reinterpret_cast<const uint4*>(prm.v + t * prm.v_st[2] + head * prm.v_st[1]) + part;
+#pragma unroll
+        for (int p = 0; p < P; ++p) { k[p] = __ldcs(kf + p * LANES); v[p] = __ldcs(vf + p * LANES); }
+        const int pos = paged_len(c, b) - n_new + i;
         if (pos >= 0) page = paged_page(c, b, pos);
+        at = pos & ((1 << c.page_shift) - 1);
     }
-    const bool on = page >= 0;
-    uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
-    if (on) {
-        k = __ldg(reinterpret_cast<const uint4*>(prm.k + t * prm.k_st[2] + head * prm.k_st[1]) + part);
-        v = __ldg(reinterpret_cast<const uint4*>(prm.v + t * prm.v_st[2] + head * prm.v_st[1]) + part);
-    }
-    const int at = pos & ((1 << c.page_shift) - 1);
     const int64_t ko = page * c.ks[0] + head * c.ks[1] + at * c.ks[2], vo = page * c.vs[0] + head * c.vs[1] + at * c.vs[2];
     if constexpr (INT8) {
-        float dk, dv;
-        const uint2 k8 = quantise_row<T, LANES>(k, &dk), v8 = quantise_row<T, LANES>(v, &dv);
-        if (!on) return;
-        reinterpret_cast<uint2*>(c.k_pool + ko)[part] = k8;
-        reinterpret_cast<uint2*>(c.v_pool + vo)[part] = v8;
+        uint2 k8[P], v8[P];
+        const float dk = quantise_row<T, LANES>(k, k8), dv = quantise_row<T, LANES>(v, v8);
+        if (page < 0) return;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            reinterpret_cast<uint2*>(c.k_pool + ko)[part + p * LANES] = k8[p];
+            reinterpret_cast<uint2*>(c.v_pool + vo)[part + p * LANES] = v8[p];
+        }
         if (part == 0) {
             const int64_t so = ((static_cast<int64_t>(page) * c.Hk + head) << c.page_shift) + at;
             c.k_scale[so] = dk;
             c.v_scale[so] = dv;
         }
     } else {
-        if (!on) return;
-        reinterpret_cast<uint4*>(c.k_pool + 2 * ko)[part] = k;
-        reinterpret_cast<uint4*>(c.v_pool + 2 * vo)[part] = v;
-    }
-}
-
-// A row of the cache as 16-bit values, in the lanes that hold it.
-template <class T>
-__device__ __forceinline__ uint4 dequantise8(const uint2& x, float delta) {
-    uint32_t w[4];
+        if (page < 0) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t two = (i < 2 ? x.x : x.y) >> (16 * (i & 1));
-        w[i] = act_pack2(static_cast<float>(static_cast<int8_t>(two)) * delta, static_cast<float>(static_cast<int8_t>(two >> 8)) * delta, T());
+        for (int p = 0; p < P; ++p) {
+            reinterpret_cast<uint4*>(c.k_pool + 2 * ko)[part + p * LANES] = k[p];
+            reinterpret_cast<uint4*>(c.v_pool + 2 * vo)[part + p * LANES] = v[p];
+        }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Rows of the cache out.  Packed outputs: row = (token, head), heads innermost; dense ones: (sequence, head, token).
+// (The pools are read past L1: the kernel in front may have written them, and nothing is read twice.)
 template <class T, int D, bool INT8>
 __global__ void __launch_bounds__(kMoveThreads)
 paged_gather_kernel(const MoveParams prm) {
-    constexpr int LANES = D / 8, ROWS = kMoveThreads / LANES;
+    constexpr int P = kPieces, LANES = D / 8 / P, ROWS = kMoveThreads / LANES;
     const PagedCache& c = prm.c;
     const int row = blockIdx.x * ROWS + threadIdx.x / LANES, part = threadIdx.x % LANES;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
     int b, head, i, dst;            // dst: token of the output (packed), or i
     if (prm.cu != nullptr) {
         const int t = row / c.Hk;
@@ -242,46 +265,63 @@ paged_gather_kernel(const MoveParams prm) {
     if (row >= prm.rows || b >= c.B || i < 0) return;
     const int len = paged_len(c, b), first = prm.start != nullptr ? max(prm.start[b], 0) : 0;
     if (i >= len - first) return;
-    const int pos = first + i;
-    const int page = paged_page(c, b, pos);
-    uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
+    const int pos = first + i, page = paged_page(c, b, pos);
+    uint4 k[P], v[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) k[p] = v[p] = make_uint4(0u, 0u, 0u, 0u);
     if (page >= 0) {
         const int at = pos & ((1 << c.page_shift) - 1);
         const int64_t ko = page * c.ks[0] + head * c.ks[1] + at * c.ks[2], vo = page * c.vs[0] + head * c.vs[1] + at * c.vs[2];
         if constexpr (INT8) {
             const int64_t so = ((static_cast<int64_t>(page) * c.Hk + head) << c.page_shift) + at;
-            k = dequantise8<T>(__ldg(reinterpret_cast<const uint2*>(c.k_pool + ko) + part), c.k_scale[so]);
-            v = dequantise8<T>(__ldg(reinterpret_cast<const uint2*>(c.v_pool + vo) + part), c.v_scale[so]);
+            uint2 k8[P], v8[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                k8[p] = __ldcg(reinterpret_cast<const uint2*>(c.k_pool + ko) + part + p * LANES);
+                v8[p] = __ldcg(reinterpret_cast<const uint2*>(c.v_pool + vo) + part + p * LANES);
+            }
+            const float dk = __ldcg(c.k_scale + so), dv = __ldcg(c.v_scale + so);
+#pragma unroll
+            for (int p = 0; p < P; ++p) { k[p] = dequantise8<T>(k8[p], dk); v[p] = dequantise8<T>(v8[p], dv); }
         } else {
-            k = __ldg(reinterpret_cast<const uint4*>(c.k_pool + 2 * ko) + part);
-            v = __ldg(reinterpret_cast<const uint4*>(c.v_pool + 2 * vo) + part);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                k[p] = __ldcg(reinterpret_cast<const uint4*>(c.k_pool + 2 * ko) + part + p * LANES);
+                v[p] = __ldcg(reinterpret_cast<const uint4*>(c.v_pool + 2 * vo) + part + p * LANES);
+            }
         }
     }
     const int64_t batch = prm.cu != nullptr ? 0 : b;
-    reinterpret_cast<uint4*>(prm.k + batch * prm.k_st[0] + head * prm.k_st[1] + dst * prm.k_st[2])[part] = k;
-    reinterpret_cast<uint4*>(prm.v + batch * prm.v_st[0] + head * prm.v_st[1] + dst * prm.v_st[2])[part] = v;
+    uint4* kt = reinterpret_cast<uint4*>(prm.k + batch * prm.k_st[0] + head * prm.k_st[1] + dst * prm.k_st[2]) + part;
+    uint4* vt = reinterpret_cast<uint4*>(prm.v + batch * prm.v_st[0] + head * prm.v_st[1] + dst * prm.v_st[2]) + part;
+#pragma unroll
+    for (int p = 0; p < P; ++p) { __stcs(kt + p * LANES, k[p]); __stcs(vt + p * LANES, v[p]); }
 }
 
-using MoveKernel = void (*)(const MoveParams);
-
-int launch_move(MoveKernel kernel, const MoveParams& prm, cudaStream_t stream) {
-    const int rows_per_cta = kMoveThreads / (prm.c.d / 8);
-    kernel<<<static_cast<unsigned>(ceil_div(prm.rows, rows_per_cta)), kMoveThreads, 0, stream>>>(prm);
-    g_launch_count.fetch_add(1);
-    return static_cast<int>(cudaGetLastError());
-}
-
-// (a 16-bit cache is copied, whatever its type)
+// (a 16-bit cache is copied, whatever its type; programmatic dependent launch: the launch overlaps the kernel in front, whose
+// end both kernels wait for)
 template <bool APPEND, class T, int D>
-MoveKernel pick_move(bool int8) {
-    if constexpr (APPEND) return int8 ? paged_append_kernel<T, D, true> : paged_append_kernel<__half, D, false>;
-    else return int8 ? paged_gather_kernel<T, D, true> : paged_gather_kernel<__half, D, false>;
+int launch_move(bool int8, const MoveParams& prm, cudaStream_t stream) {
+    void (*kernel)(const MoveParams);
+    if constexpr (APPEND) kernel = int8 ? paged_append_kernel<T, D, true> : paged_append_kernel<__half, D, false>;
+    else kernel = int8 ? paged_gather_kernel<T, D, true> : paged_gather_kernel<__half, D, false>;
+    constexpr int kRows = kMoveThreads / (D / 8 / kPieces);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(ceil_div(prm.rows, kRows))); cfg.blockDim = dim3(kMoveThreads); cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, prm);
+    g_launch_count.fetch_add(1);
+    return static_cast<int>(e);
 }
 template <bool APPEND>
-MoveKernel pick_move(const tilemix_paged_t* p) {
+int launch_move(const tilemix_paged_t* p, const MoveParams& prm, cudaStream_t stream) {
     const bool int8 = p->cache_type == TILEMIX_CACHE_INT8;
-    if (p->act_type == TILEMIX_TYPE_FP16) return p->head_dim == 128 ? pick_move<APPEND, __half, 128>(int8) : pick_move<APPEND, __half, 64>(int8);
-    return p->head_dim == 128 ? pick_move<APPEND, __nv_bfloat16, 128>(int8) : pick_move<APPEND, __nv_bfloat16, 64>(int8);
+    if (p->act_type == TILEMIX_TYPE_FP16)
+        return p->head_dim == 128 ? launch_move<APPEND, __half, 128>(int8, prm, stream) : launch_move<APPEND, __half, 64>(int8, prm, stream);
+    return p->head_dim == 128 ? launch_move<APPEND, __nv_bfloat16, 128>(int8, prm, stream) : launch_move<APPEND, __nv_bfloat16, 64>(int8, prm, stream);
 }
 
 // Byte strides (batch, head, token) of the 16-bit side.  Only outputs must not overlap themselves.
@@ -330,7 +370,7 @@ int tilemix_paged_append(const tilemix_paged_t* p, int32_t n_tokens, const void*
     prm.cu = cu_new;
     prm.k = static_cast<uint8_t*>(const_cast<void*>(k_new));
     prm.v = static_cast<uint8_t*>(const_cast<void*>(v_new));
-    return launch_move(pick_move<true>(p), prm, static_cast<cudaStream_t>(stream));
+    return launch_move<true>(p, prm, static_cast<cudaStream_t>(stream));
 }
 
 int tilemix_paged_gather(const tilemix_paged_t* p, const int32_t* start, const int32_t* cu_out, int32_t out_rows, void* k_out,
@@ -355,7 +395,7 @@ int tilemix_paged_gather(const tilemix_paged_t* p, const int32_t* start, const i
     prm.out_rows = out_rows;
     prm.k = static_cast<uint8_t*>(k_out);
     prm.v = static_cast<uint8_t*>(v_out);
-    return launch_move(pick_move<false>(p), prm, static_cast<cudaStream_t>(stream));
+    return launch_move<false>(p, prm, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"
