@@ -487,7 +487,7 @@ _ACT = {torch.float16: TYPE_FP16, torch.bfloat16: TYPE_BF16}
 
 class PagedCache:
     """A layer's paged cache, as paged_cache() describes it; keeps the tensors alive that the C struct points to."""
-    __slots__ = ("struct", "ref", "tensors", "dtype", "device")
+    __slots__ = ("struct", "ref", "tensors", "dtype", "device", "index", "batch", "heads_kv", "head_dim")
 
 
 def paged_cache(k_pool, v_pool, block_table, cache_len, k_scale=None, v_scale=None, dtype=None) -> PagedCache:
@@ -520,61 +520,64 @@ def paged_cache(k_pool, v_pool, block_table, cache_len, k_scale=None, v_scale=No
     c.struct.k_pool, c.struct.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
     c.struct.k_scale, c.struct.v_scale = _ptr(k_scale), _ptr(v_scale)
     c.struct.block_table, c.struct.cache_len = block_table.data_ptr(), cache_len.data_ptr()
-    c.ref, c.tensors, c.dtype, c.device = ctypes.byref(c.struct), tuple(held), dtype, dev
+    c.ref, c.tensors, c.dtype, c.device, c.index = ctypes.byref(c.struct), tuple(held), dtype, dev, dev.index
+    c.batch, c.heads_kv, c.head_dim = B, hk, d
     return c
 
 
-def _paged_side(c, t, dims, what):
-    """Checks a 16-bit tensor next to the cache; returns its strides for the C call (None where it is dense)."""
-    assert t.dtype == c.dtype and t.device == c.device and t.shape[-1] == c.struct.head_dim and t.dim() == dims, what
-    if t.is_contiguous():
-        return None
+# A decode step of a short context is bound by what these calls spend on the host (append 5.6 us, 3.3 of them in the library and
+# the driver), hence few attribute look-ups and no arguments built where a tensor is dense.
+
+def _paged_strides(t):
     st = t.stride()
     assert st[-1] == 1, "head_dim axis must be contiguous"
     return (ctypes.c_int64 * 3)(*st[:-1])
 
 
 def _paged_index(c, t, n):
-    if t is not None:
-        assert t.dtype == torch.int32 and t.device == c.device and t.shape == (n,) and t.is_contiguous()
-    return _ptr(t)
+    assert t.dtype is torch.int32 and t.device == c.device and t.shape == (n,) and t.is_contiguous()
+    return t.data_ptr()
 
 
-def _paged_call(c, name, *args):
+def _paged_call(c, name, fn, *args):
     """The C call on the current stream of the cache's device."""
-    if c.device.index != torch._C._cuda_getDevice():
-        with torch.cuda.device(c.device):
-            rc = getattr(lib(), name)(c.ref, *args, _stream())
+    if c.index == torch._C._cuda_getDevice():
+        rc = fn(c.ref, *args, torch._C._cuda_getCurrentRawStream(c.index))
     else:
-        rc = getattr(lib(), name)(c.ref, *args, _stream())
-    _check(rc, name)
+        with torch.cuda.device(c.device):
+            rc = fn(c.ref, *args, torch._C._cuda_getCurrentRawStream(c.index))
+    if rc != OK:
+        raise TilemixError(rc, name)
 
 
 def tilemix_paged_append(c: PagedCache, k_new, v_new, cu_new=None):
     """Writes the new tokens k_new, v_new [n,Hk,d] into the cache, as the last ones of their sequences (cache_len counts them
     already); cu_new int32 [B+1] (CUDA) says whose rows they are, None: one a sequence."""
-    assert k_new.shape == v_new.shape and k_new.shape[1] == c.struct.heads_kv
-    ks, vs = _paged_side(c, k_new, 3, "k_new"), _paged_side(c, v_new, 3, "v_new")
-    _paged_call(c, "tilemix_paged_append", k_new.shape[0], k_new.data_ptr(), ks, v_new.data_ptr(), vs,
-                _paged_index(c, cu_new, c.struct.batch + 1))
+    n, hk, d = k_new.shape
+    assert hk == c.heads_kv and d == c.head_dim and v_new.shape == k_new.shape
+    assert k_new.dtype is c.dtype and v_new.dtype is c.dtype and k_new.device == c.device and v_new.device == c.device
+    _paged_call(c, "tilemix_paged_append", lib().tilemix_paged_append, n,
+                k_new.data_ptr(), None if k_new.is_contiguous() else _paged_strides(k_new),
+                v_new.data_ptr(), None if v_new.is_contiguous() else _paged_strides(v_new),
+                None if cu_new is None else _paged_index(c, cu_new, c.batch + 1))
 
 
 def tilemix_paged_gather(c: PagedCache, k_out, v_out, start=None, cu_out=None):
     """Reads tokens [start, cache_len) of every sequence back into k_out, v_out: dense [B,Hk,n,d], or with cu_out (int32 [B+1],
     CUDA) packed [n,Hk,d].  Rows that no token belongs to are left as they were.  Returns (k_out, v_out)."""
-    s = c.struct
-    assert k_out.shape == v_out.shape
-    dims = 4 if cu_out is None else 3
-    ks, vs = _paged_side(c, k_out, dims, "k_out"), _paged_side(c, v_out, dims, "v_out")
     if cu_out is None:
-        assert k_out.shape[0] == s.batch and k_out.shape[1] == s.heads_kv
-        n = k_out.shape[2]
+        B, hk, n, d = k_out.shape
+        assert B == c.batch
     else:
-        assert k_out.shape[1] == s.heads_kv
-        n = k_out.shape[0]
+        n, hk, d = k_out.shape
+    assert hk == c.heads_kv and d == c.head_dim and v_out.shape == k_out.shape
+    assert k_out.dtype is c.dtype and v_out.dtype is c.dtype and k_out.device == c.device and v_out.device == c.device
+    ks = None if k_out.is_contiguous() else _paged_strides(k_out)
+    vs = None if v_out.is_contiguous() else _paged_strides(v_out)
+    if cu_out is not None:
         ks, vs = (st and (ctypes.c_int64 * 3)(0, st[1], st[0]) for st in (ks, vs))     # (batch, head, token)
-    _paged_call(c, "tilemix_paged_gather", _paged_index(c, start, s.batch), _paged_index(c, cu_out, s.batch + 1), n,
-                k_out.data_ptr(), ks, v_out.data_ptr(), vs)
+    _paged_call(c, "tilemix_paged_gather", lib().tilemix_paged_gather, None if start is None else _paged_index(c, start, c.batch),
+                None if cu_out is None else _paged_index(c, cu_out, c.batch + 1), n, k_out.data_ptr(), ks, v_out.data_ptr(), vs)
     return k_out, v_out
 
 
@@ -584,19 +587,20 @@ def tilemix_paged_decode_workspace_size(c: PagedCache, heads_q: int) -> int:
 
 def tilemix_paged_decode(c: PagedCache, q, out=None, want_lse=False, softmax_scale=0.0, workspace=None):
     """One decode step: q [B,Hq,d] attends to the cache.  Returns a dict: out [B,Hq,d], lse [B,Hq] FP32 (if asked), workspace."""
-    s = c.struct
-    assert q.shape[0] == s.batch
-    qs = _paged_side(c, q, 3, "q")
-    hq = q.shape[1]
+    B, hq, d = q.shape
+    assert B == c.batch and d == c.head_dim and q.dtype is c.dtype and q.device == c.device
     if out is None:
-        out = torch.empty((s.batch, hq, s.head_dim), dtype=c.dtype, device=c.device)
-    assert out.shape == q.shape
-    os_ = _paged_side(c, out, 3, "out")
-    lse = torch.empty((s.batch, hq), dtype=torch.float32, device=c.device) if want_lse else None
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        os_ = None
+    else:
+        assert out.shape == q.shape and out.dtype is c.dtype and out.device == c.device
+        os_ = None if out.is_contiguous() else _paged_strides(out)
+    lse = torch.empty((B, hq), dtype=torch.float32, device=c.device) if want_lse else None
     if workspace is None:
-        workspace = torch.empty(max(tilemix_paged_decode_workspace_size(c, hq), 16), dtype=torch.uint8, device=c.device)
+        workspace = torch.empty(tilemix_paged_decode_workspace_size(c, hq), dtype=torch.uint8, device=c.device)
     else:
         assert workspace.device == c.device and workspace.is_contiguous()
-    _paged_call(c, "tilemix_paged_decode", hq, softmax_scale, q.data_ptr(), qs, out.data_ptr(), os_, _ptr(lse),
-                workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _paged_call(c, "tilemix_paged_decode", lib().tilemix_paged_decode, hq, softmax_scale, q.data_ptr(),
+                None if q.is_contiguous() else _paged_strides(q), out.data_ptr(), os_, None if lse is None else lse.data_ptr(),
+                workspace.data_ptr(), workspace.nbytes)
     return {"out": out, "lse": lse, "workspace": workspace}
