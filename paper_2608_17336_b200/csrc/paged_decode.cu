@@ -64,20 +64,15 @@ struct PoolMaps {
 template <class T, int D, bool INT8, int NB>
 struct Cfg {
     static constexpr int kElt = INT8 ? 1 : 2;
-    // Warps of a CTA and stages of their rings.  The INT8 form is bound by issue slots and latencies, not by bytes, unless many
-    // warps share them (8 x 32K keys, d = 128: four a CTA 135 us, eight 101); sixteen query heads need the registers of six.
-#ifndef CFG_X
-#define I1S 2
-#define I1C 3
-#define I1B 8192
-#define I2S 3
-#define I2C 2
-#define I2B 8192
-#endif
+    // Warps of a CTA, stages of their rings, CTAs of an SM.  The INT8 form is bound by issue slots before bytes unless the cost of
+    // a chunk (its copies, its wait, the look at the maxima) is spread over 32 keys: eight warps with chunks of 16 keys need 495
+    // instructions for 16 keys, four with 32 need 349.  Sixteen query heads take the registers of a third CTA.  (us, three
+    // CTAs of two stages and two of three: 64 ragged FP16 contexts, heads of 64 96 / 100, 64 short ones of 128 35 / 39, 16 x 32K
+    // BF16 equal; 256 short INT8 ones 25 / 36.)
     static constexpr int W = 4;
-    static constexpr int kStages = INT8 ? (NB == 1 ? I1S : I2S) : 3;
-    static constexpr int kCtasPerSm = INT8 ? (NB == 1 ? I1C : I2C) : 2;
-    static constexpr int kStageBytes = INT8 ? (NB == 1 ? I1B : I2B) : 8192;
+    static constexpr int kStages = NB == 1 ? 2 : 3;
+    static constexpr int kCtasPerSm = NB == 1 ? 3 : 2;
+    static constexpr int kStageBytes = 8192;
     static constexpr int kRingBytes = W * kStages * kStageBytes;
     static constexpr int kMinTeam = 2;                              // see find_work
     static constexpr int kThreads = 32 * W;
