@@ -843,7 +843,9 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 }
 
 // Joins the parts of the rows that several workers shared.  A job (row, s, w, n) names slot s and the first slots of n workers
-// from w on.  What bounds it is the round trips: the parts are loaded kJoinAtOnce at a time.  A row of up to that many has a
+// from w on.  (A kernel of its own, whose launch overlaps the step: the last CTA of a row joining it at its end, found by a
+// counter or by words that the others set, waits for fences and atomics longer than a grid does for its predecessor: one
+// sequence of 500 keys 6.6 us so, 11.0 and 9.0 that way, 8 x 32 K 98, 104, 104.)  What bounds it is the round trips: the parts are loaded kJoinAtOnce at a time.  A row of up to that many has a
 // warp for every fragment; the parts of others are shared out over the warps, fragment by fragment (by a block each where rows
 // are few).
 constexpr int kJoinAtOnce = 8;
@@ -1017,7 +1019,7 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     // warps of one block (64 rows of seven parts: 1.5 us so, 7 in large blocks, which an SM holds one of)
     const bool few = prm.jobs_by_row && static_cast<int64_t>(plan.jobs) * kJoinAtOnce < plan.ctas;
     constexpr int kFew = 16, kMany = 4, F = (D / 16) * NB;
-    cfg.gridDim = dim3(plan.jobs, few ? F : plan.jobs <= kSms ? F / kMany : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
+    cfg.gridDim = dim3(plan.jobs, few ? F : plan.jobs * (F / kMany) <= 5 * kSms ? F / kMany : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
     e = few ? cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kFew>, prm) : cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kMany>, prm);
     g_launch_count.fetch_add(1);
     return static_cast<int>(e);

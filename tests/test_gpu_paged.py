@@ -364,6 +364,59 @@ def test_bounded_waits(act, int8, hq):
     ref.check_decode(s, q, again)
 
 
+def test_decode_calls_share_a_workspace_in_turn():
+    """Calls of other shapes, and two captured graphs, one after the other on one workspace: what one leaves there says nothing
+    to the next."""
+    t = tm()
+    cases = []
+    for i, (d, hk, hq, lens) in enumerate([(128, 2, 8, [3000, 5]), (64, 4, 16, [100] * 40), (128, 8, 64, [700, 900]), (64, 1, 16, [9000])]):
+        s = ref.Setup("fp16", True, d, 16, hk, lens, seed=i, device=DEV)
+        cases.append((s.cache(), query(s, hq, seed=i), s))
+    ws = torch.full((max(t.tilemix_paged_decode_workspace_size(c, q.shape[1]) for c, q, _ in cases),), 173, dtype=torch.uint8, device=DEV)
+    want = [t.tilemix_paged_decode(c, q)["out"] for c, q, _ in cases]
+    graphs, outs = [], []
+    for c, q, _ in cases:
+        out = torch.empty_like(q)
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            t.tilemix_paged_decode(c, q, out=out, workspace=ws)
+        graphs.append(g)
+        outs.append(out)
+    for _ in range(3):
+        for (c, q, s), w in zip(cases, want):
+            assert torch.equal(t.tilemix_paged_decode(c, q, workspace=ws)["out"], w)
+        for g, o, w in zip(graphs, outs, want):
+            o.zero_()
+            g.replay()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o, w)
+    for (c, q, s), w in zip(cases, want):
+        ref.check_decode(s, q, {"out": w, "lse": None})
+
+
+def test_decode_on_two_streams_at_once():
+    """Two calls that overlap, each with its own workspace."""
+    t = tm()
+    cases = []
+    for i in range(2):
+        s = ref.Setup("bf16", i == 0, 128, 16, 4, [4000, 100, 2500], seed=i, device=DEV)
+        cases.append((s.cache(), query(s, 16, seed=i)))
+    want = [t.tilemix_paged_decode(c, q)["out"] for c, q in cases]
+    ws = [torch.empty(t.tilemix_paged_decode_workspace_size(c, 16), dtype=torch.uint8, device=DEV) for c, _ in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(30):
+        for i, (c, q) in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(t.tilemix_paged_decode(c, q, workspace=ws[i])["out"])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i])
+
+
 # ---------------------------------------------------------------------------------------------------- together
 
 @pytest.mark.parametrize("act,int8", KINDS)
