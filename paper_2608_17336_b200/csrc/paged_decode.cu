@@ -92,6 +92,11 @@ struct Cfg {
     static constexpr float kOff = kHalfP ? 14.f : 0.f;
     static constexpr float kUnOff = kHalfP ? 6.103515625e-5f : 1.f;
     static constexpr float kLine = kHalfP ? 1.5f : 8.f;
+    // A probability goes to the tensor cores as two 16-bit numbers, what the first leaves out being the second, so that the
+    // error of an output is that of its own rounding (one number: 1.4 times that; an eighth more MMAs and a few conversions:
+    // 8 x 32K keys equal, 256 short INT8 sequences 24.8 -> 25.5 us, 32 x 4K INT8 ones 36 -> 39).  Not where FP16
+    // probabilities make BF16 outputs: one number has three bits more than the output.
+    static constexpr bool kTwoHalves = !(INT8 && std::is_same<T, __nv_bfloat16>::value);
     static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
 };
 constexpr float kNoMax = -1e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
@@ -296,6 +301,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     using C = Cfg<T, D, INT8, NB>;
     constexpr int CH = C::CH, MB = C::MB, W = C::W, kStages = C::kStages, kStageBytes = C::kStageBytes;
     constexpr bool BF16 = !C::kHalfP;
+    constexpr bool TWO_P = C::kTwoHalves;
     extern __shared__ uint8_t smem[];
     __shared__ __align__(8) uint64_t full_bar[W][kStages];
     __shared__ uint32_t hole_s[W][kStages];                          // bit 4 i: the 16 keys i of the chunk lie in a hole
@@ -539,10 +545,10 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 constexpr bool PART = decltype(part)::value;
                 const uint32_t kst = ring_u32 + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128)), vst = kst + C::kVOff;
                 const uint8_t* const st = stages + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128));
-                // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same).  Two sums, of the even and the odd
-                // steps: the chain of MMAs that wait for one another is half as long.
-                float sc[BLOCKS][NB][4], v_mul[BLOCKS][2];
-                float odd[BLOCKS][NB][4];
+                // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same).  A block alone sums its even and its
+                // odd steps apart: the chain of MMAs that wait for one another is half as long.
+                constexpr bool TWO = BLOCKS * NB == 1;
+                float sc[BLOCKS][NB][4], v_mul[BLOCKS][2], odd[BLOCKS][NB][4];
 #pragma unroll
                 for (int mb = 0; mb < BLOCKS; ++mb)
 #pragma unroll
@@ -564,7 +570,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                                 const uint32_t a1 = codes_to_half2<false>(ub), a3 = codes_to_half2<true>(ub);
 #pragma unroll
                                 for (int nb = 0; nb < NB; ++nb)
-                                    mma_16816<false>(w & 1 ? odd[mb][nb] : sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
+                                    mma_16816<false>(TWO && (w & 1) ? odd[mb][nb] : sc[mb][nb], a0, a1, a2, a3, qf[nb][4 * j + w][0], qf[nb][4 * j + w][1]);
                             }
                         }
                     } else {
@@ -575,7 +581,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                             ldmatrix_x4<false>(a, kst + value_piece<CH>(row, 2 * i + piece));
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb)
-                                mma_16816<BF16>(i & 1 ? odd[mb][nb] : sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
+                                mma_16816<BF16>(TWO && (i & 1) ? odd[mb][nb] : sc[mb][nb], a[0], a[1], a[2], a[3], qf[nb][i][0], qf[nb][i][1]);
                         }
                     }
                 }
@@ -590,7 +596,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                sc[mb][nb][2 * i + k] += odd[mb][nb][2 * i + k];
+                                if constexpr (TWO) sc[mb][nb][2 * i + k] += odd[mb][nb][2 * i + k];
                                 if constexpr (INT8) sc[mb][nb][2 * i + k] *= dk;
                             }
                     }
@@ -682,7 +688,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 // ---- probabilities, and O^T += V^T P^T block by block
 #pragma unroll
                 for (int mb = 0; mb < BLOCKS; ++mb) {
-                    uint32_t p0[NB], p1[NB];
+                    uint32_t p0[NB], p1[NB], r0[NB], r1[NB];
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         float p[4];
@@ -693,8 +699,14 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                             if constexpr (INT8) p[k] *= v_mul[mb][k >> 1] * inv;
                         }
                         using P = typename std::conditional<C::kHalfP, __half, __nv_bfloat16>::type;
-                        p0[nb] = transpose_8x8(act_pack2(p[0], p[1], P()));
-                        p1[nb] = transpose_8x8(act_pack2(p[2], p[3], P()));
+                        const uint32_t h0 = act_pack2(p[0], p[1], P()), h1 = act_pack2(p[2], p[3], P());
+                        p0[nb] = transpose_8x8(h0);
+                        p1[nb] = transpose_8x8(h1);
+                        if constexpr (TWO_P) {
+                            const float2 f0 = act_to_float2(h0, P()), f1 = act_to_float2(h1, P());
+                            r0[nb] = transpose_8x8(act_pack2(p[0] - f0.x, p[1] - f0.y, P()));
+                            r1[nb] = transpose_8x8(act_pack2(p[2] - f1.x, p[3] - f1.y, P()));
+                        }
                     }
                     if constexpr (INT8) {
                         // keys of columns 2 t, 2 t + 1 (and + 8) of V^T: four rows, of which this lane takes D / 8 columns
@@ -722,7 +734,10 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                                 const uint32_t a0 = codes_to_half2<false>(a01), a1 = codes_to_half2<true>(a01);
                                 const uint32_t a2 = codes_to_half2<false>(a23), a3 = codes_to_half2<true>(a23);
 #pragma unroll
-                                for (int nb = 0; nb < NB; ++nb) mma_16816<false>(acc[2 * w + h][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
+                                for (int nb = 0; nb < NB; ++nb) {
+                                    mma_16816<false>(acc[2 * w + h][nb], a0, a1, a2, a3, p0[nb], p1[nb]);
+                                    if constexpr (TWO_P) mma_16816<false>(acc[2 * w + h][nb], a0, a1, a2, a3, r0[nb], r1[nb]);
+                                }
                             }
                         }
                     } else {
@@ -732,7 +747,10 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                             uint32_t a[4];
                             ldmatrix_x4<true>(a, vst + value_piece<CH>(row, 2 * md + piece));
 #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
+                            for (int nb = 0; nb < NB; ++nb) {
+                                mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], p0[nb], p1[nb]);
+                                if constexpr (TWO_P) mma_16816<BF16>(acc[md][nb], a[0], a[1], a[2], a[3], r0[nb], r1[nb]);
+                            }
                         }
                     }
                 }

@@ -102,14 +102,17 @@ class Setup:
 def attend(s, q, scale=0.0):
     """float64 (out [B,Hq,d], lse [B,Hq]) and bounds of what the kernel may be off by, from the arithmetic it states.
 
-    u = half a step of the 16-bit type: outputs are rounded (u |o|) and so are the probabilities (u A, A = sum p |v|; those
-    below 2^-28 of the largest are subnormal FP16: at most 2^-39 of the largest each).  A score of magnitude S (sum of |q_i k_i|,
+    u = half a step of the 16-bit type: outputs are rounded (u |o|).  A probability is a sum of two 16-bit numbers, the second
+    the first's rounding error, rounded (u^2 of it; in all u^2 A, A = sum p |v|), over INT8 caches in FP16, and one FP16
+    number where the outputs are BF16 (2^-11); those below 2^-28 of the largest are subnormal FP16 (at most 2^-39 of the
+    largest each).  A score of magnitude S (sum of |q_i k_i|,
     log2 units) is off by at most (d + 8) 2^-23 S (FP32 products summed in any order, each sum rounded to nearest or
     towards zero; scales), the exponential by 2^-22, FP32 sums over n keys by n 2^-24: relative errors of p of at most e,
     hence 2 e A (numerator and denominator)."""
     B, hq, d = q.shape
     scale = scale or 1 / math.sqrt(d)
     u = torch.finfo(s.act).eps / 2
+    up = 2.0 ** -11 if s.int8 and s.act == torch.bfloat16 else u * u
     out, lse = np.zeros((B, hq, d)), np.full((B, hq), -np.inf)
     tol, tol_lse = np.zeros((B, hq, d)), np.zeros((B, hq))
     qd = f64(q)
@@ -130,7 +133,7 @@ def attend(s, q, scale=0.0):
             big = (np.abs(kk) @ np.abs(qd[b, h])).max() * scale * math.log2(math.e)
             e = (d + 8) * 2.0 ** -23 * big + 2.0 ** -22 + n * 2.0 ** -24
             mass = (p / z) @ np.abs(vv)
-            tol[b, h] = u * np.abs(out[b, h]) + (u + 2 * e) * 1.01 * mass + n * 2.0 ** -39 * np.abs(vv).max() / z
+            tol[b, h] = u * np.abs(out[b, h]) + (up + 2 * e) * 1.01 * mass + n * 2.0 ** -39 * np.abs(vv).max() / z
             tol_lse[b, h] = e + 2.0 ** -22 * (abs(lse[b, h]) + big)
     return out, lse, tol + torch.finfo(s.act).tiny * u, tol_lse
 
