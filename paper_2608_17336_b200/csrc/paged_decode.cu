@@ -80,6 +80,11 @@ struct Cfg {
     static constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
     static_assert(CH == 1 << kChShift, "chunks are whole boxes");
     static constexpr int MB = CH / 16;                              // blocks of 16 keys
+    // Blocks that a warp takes together, where a chunk has them whole: what does not depend on their number is done once for two,
+    // in twice the code and more registers.  (us together and one by one: 64 ragged FP16 steps, heads of 64 97 / 98, 16 x 8K
+    // INT8, heads of 64 32.6 / 36.6, 1 x 128K INT8, sixteen query heads 27.3 / 28.7; but 8 x 32K INT8, heads of 128 98.7 / 92.8,
+    // 64 x 500 29.3 / 27.6.)
+    static constexpr int kTogether = MB == 1 || (INT8 && NB == 1 && D == 128) ? 1 : 2;
     static constexpr int kVOff = CH * D * kElt;                     // values behind the keys of a stage
     static constexpr int kBoxCols = INT8 ? 1 : D / 64;              // boxes side by side in a row of 16-bit values
     static constexpr int kScaleBytes = INT8 ? W * kStages * CH * 8 : 0;
@@ -601,7 +606,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                             }
                     }
                 // ---- keys past the end and in holes do not exist, whatever lies in their rows
-                if constexpr (PART) {
+                if (PART && (live < 16 * first_mb + 16 || holes != 0u)) {
                     const bool hole = (holes >> (4 * first_mb)) & 1u;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -755,7 +760,9 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                     }
                 }
             };
-            if (live == CH && holes == 0u) attend(std::integral_constant<int, MB>(), std::false_type(), 0);
+            if (C::kTogether > 1 && live == CH && holes == 0u)
+#pragma unroll 1
+                for (int mb = 0; mb < MB; mb += C::kTogether) attend(std::integral_constant<int, C::kTogether>(), std::false_type(), mb);
             else
 #pragma unroll 1
                 for (int mb = 0; 16 * mb < live; ++mb) attend(std::integral_constant<int, 1>(), std::true_type(), mb);
