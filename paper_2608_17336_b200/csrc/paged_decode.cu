@@ -42,6 +42,7 @@ constexpr int kSms = 148;
 struct PagedDecodeParams {
     PagedCache c;
     int Hq, R;                      // query heads, query heads per KV head
+    int wave, jobs;                 // CTAs that run at the same time; jobs of the joining kernel
     int groups, HG;                 // groups of up to 8 NB query heads per KV head; rows of a sequence (Hk * groups)
     float scale_log2;
     const uint8_t* q;
@@ -176,24 +177,44 @@ __device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm
 
 // What a warp has to do.  A worker is a team of the CTA's warps: all of them, or, where there are rows enough for more workers
 // and the rows are short (fewer than kShortRow chunks a warp of the team on average), half of them.  Chunks are CH keys, or
-// fewer where there would be fewer units than CTAs.  A unit is a chunk for each warp of the team; the U units go to n workers,
-// U / n or one more to each.
+// fewer where there would be fewer units than CTAs.  A unit is a chunk for each warp of the team; the U units go to n workers in
+// shares of U / n or one more (and a long share to two workers, see below).
 struct Work {
     Cursor at;
     int team_shift, chunk_shift, worker;
-    int base, longer;                        // units of a worker; the first `longer` workers have one more
+    int base, longer;                        // units of a share; the first `longer` shares have one more
+    int pieces_shift, small;                 // pieces of a share: the first, and others of `small` units
 
-    __device__ __forceinline__ int first_of(int w) const { return w * base + min(w, longer); }
+    __device__ __forceinline__ int share_first(int i) const { return i * base + min(i, longer); }
+    __device__ __forceinline__ int units_of(int w) const {
+        if ((w & ((1 << pieces_shift) - 1)) != 0) return small;
+        return base + ((w >> pieces_shift) < longer ? 1 : 0) - ((1 << pieces_shift) - 1) * small;
+    }
+    __device__ __forceinline__ int first_of(int w) const {
+        const int i = w >> pieces_shift, j = w & ((1 << pieces_shift) - 1);
+        return j == 0 ? share_first(i) : share_first(i + 1) - ((1 << pieces_shift) - j) * small;
+    }
     __device__ __forceinline__ int worker_of(int unit) const {
-        const int split = longer * (base + 1);
-        return unit < split ? unit / (base + 1) : longer + (unit - split) / base;
+        const int split = longer * (base + 1), i = unit < split ? unit / (base + 1) : longer + (unit - split) / base;
+        int w = i << pieces_shift;
+        if (pieces_shift != 0) {
+            const int behind = unit - (share_first(i + 1) - ((1 << pieces_shift) - 1) * small);
+            if (behind >= 0) w += 1 + behind / small;
+        }
+        return w;
     }
 };
 constexpr int kShortRow = 4;
-template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE>
+// SMs do not get the same share of the memory's bandwidth (equal shares of 8 x 32K keys end after 70 to 92 us, in the order of
+// their SMs' clusters).  Of long shares of a 16-bit cache the last eighth is a worker of its own, which goes to the SM that is
+// done first: blocks behind the first wave.  (us without and with: 64 ragged FP16 steps, heads of 64 97.4 / 92.8, 16 x 32K BF16
+// 161.2 / 159.7; a block's entry costs as much as that gains where shares are short, 16 x 4K BF16, sixteen query heads
+// 37.1 / 42.9, and in the INT8 form, 8 x 32K 93.2 / 97.0.)
+constexpr int kPiecesShift = 1, kLongShare = 32;
+template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE, bool PIECES>
 __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     constexpr int kTeamShift = W == 8 ? 3 : 2, kMinShift = MIN_TEAM == 2 ? 1 : 2;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = prm.c.B, ctas = gridDim.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = prm.c.B, ctas = prm.wave;
     // (the lengths of the first 256 sequences stay in registers: the loads wait for memory once)
     constexpr int kKept = 8;
     int kept[kKept];
@@ -218,9 +239,17 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     const int unit_shift = w.chunk_shift + w.team_shift;
     auto units_of = [&](int len) { return (len + (1 << unit_shift) - 1) >> unit_shift; };
     const int U = __reduce_add_sync(0xffffffffu, sum_of(units_of)) * prm.HG, n = min(ctas << (kTeamShift - w.team_shift), U);
-    w.worker = (blockIdx.x << (kTeamShift - w.team_shift)) + (warp >> w.team_shift);
-    if (w.worker >= n) return w;
-    w.base = U / n; w.longer = U - w.base * n;
+    if (n > 0) { w.base = U / n; w.longer = U - w.base * n; }
+    const int block = blockIdx.x;
+    if (PIECES && gridDim.x > ctas && w.team_shift == kTeamShift && w.base >= kLongShare) {
+        w.pieces_shift = kPiecesShift;
+        w.small = w.base >> 3;
+        // (blocks behind the first wave: one small piece of every share, then the next of every share)
+        w.worker = block < ctas ? block << kPiecesShift : (block % ctas << kPiecesShift) + block / ctas;
+    } else {
+        w.worker = block < ctas ? (block << (kTeamShift - w.team_shift)) + (warp >> w.team_shift) : 0x40000000;
+        if (w.worker >= n) return w;
+    }
     Cursor& c = w.at;
     const int first = w.first_of(w.worker);
     int before = 0;                          // units of the sequences before the 32 in hand
@@ -243,7 +272,7 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
         const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - c.n_units * prm.HG);
         c.h = at / c.n_units;
         c.unit = at - c.h * c.n_units;
-        c.left = w.base + (w.worker < w.longer ? 1 : 0);
+        c.left = w.units_of(w.worker);
         return true;
     };
 #pragma unroll
@@ -326,7 +355,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     ptx::griddep_wait();                     // the cache, the lengths and the queries may be the work of the kernel before
     ptx::griddep_launch_dependents();
 
-    const Work work = find_work<W, C::kChShift, C::kMinTeam, C::kCtasPerSm * kSms>(prm);
+    const Work work = find_work<W, C::kChShift, C::kMinTeam, C::kCtasPerSm * kSms, !INT8>(prm);
     const int team = 1 << work.team_shift, member = warp & (team - 1), team_no = warp >> work.team_shift;
     const int chunk_shift = work.chunk_shift, chunk = 1 << chunk_shift, unit_shift = chunk_shift + work.team_shift, unit_keys = 1 << unit_shift;
     Cursor cc = work.at;
@@ -457,10 +486,18 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 job = make_int4(cc.b * prm.HG + cc.h, 2 * (worker - 1) + (before == row_first ? 0 : 1), worker, last - worker + 1);
             }
         }
-        if (!prm.jobs_by_row) prm.join[blockIdx.x * (W / C::kMinTeam) + team_no] = job;
-        else if (job.x >= 0) prm.join[job.x] = job;
+        // (by worker: a job each; teams that there are not, and blocks without work, write theirs too)
+        const int at = work.pieces_shift != 0 ? work.worker : static_cast<int>(blockIdx.x) * (W / C::kMinTeam) + team_no;
+        if (prm.jobs_by_row) {
+            if (job.x >= 0) prm.join[job.x] = job;
+        } else if (at < prm.jobs) {
+            prm.join[at] = job;
+        }
     }
-    if (!prm.jobs_by_row && tid > 0 && tid < W / C::kMinTeam && tid >= W / team) prm.join[blockIdx.x * (W / C::kMinTeam) + tid] = make_int4(-1, 0, 0, 0);
+    if (!prm.jobs_by_row && work.pieces_shift == 0 && tid >= W / team && tid < W / C::kMinTeam) {
+        const int at = static_cast<int>(blockIdx.x) * (W / C::kMinTeam) + tid;
+        if (at < prm.jobs) prm.join[at] = make_int4(-1, 0, 0, 0);
+    }
     // sequences without a key
     for (int b = blockIdx.x; b < c.B; b += gridDim.x) {
         if (paged_len(c, b) > 0) continue;
@@ -935,7 +972,7 @@ paged_join_kernel(const PagedDecodeParams prm) {
         rows.sums(prm, m, z, md == 0 && lane < 4);
         rows.store(md, lane, p.o);
     };
-    if (parts <= kJoinAtOnce) {
+    if (parts <= 2 * kJoinAtOnce) {
         for (int f = f_begin + warp; f < f_end; f += WARPS) finish(f, take(f, 0, 1));
         return;
     }
@@ -956,7 +993,7 @@ paged_join_kernel(const PagedDecodeParams prm) {
 
 // Shape of a launch by instance: what resolve_decode has to know of Cfg.
 struct Plan {
-    int NB, groups, HG, ctas, jobs, splits;      // splits: whether a row can have more units than one
+    int NB, groups, HG, wave, ctas, jobs, splits;      // splits: whether a row can have more units than one
     int team, workers;                           // smallest team; workers that there may be
     size_t join_bytes, mz_bytes, total;
 };
@@ -968,10 +1005,10 @@ int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* p
     const int R = heads_q / p->heads_kv;
     plan->NB = R > 8 ? 2 : 1;
     plan->groups = static_cast<int>(ceil_div(R, 8 * plan->NB));
-    int W, min_team, wave;
+    int W, ch, min_team, wave;
     auto shape = [&](auto cfg) {
         using C = decltype(cfg);
-        W = C::W; min_team = C::kMinTeam; wave = C::kCtasPerSm * kSms;
+        W = C::W; ch = C::CH; min_team = C::kMinTeam; wave = C::kCtasPerSm * kSms;
     };
     const bool int8 = p->cache_type == TILEMIX_CACHE_INT8;
     if (p->head_dim == 128) {
@@ -988,9 +1025,12 @@ int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* p
     if (static_cast<int64_t>(p->batch) * heads_q > (int64_t{1} << 30)) return TILEMIX_ERR_SHAPE;
     plan->HG = static_cast<int>(rows_each);
     const int64_t units = rows * ceil_div(c->capacity, 16 * W);       // (the kernel makes chunks as small as 16 keys)
-    plan->ctas = static_cast<int>(units < wave ? units : wave);
+    plan->wave = static_cast<int>(units < wave ? units : wave);
+    // blocks behind the first wave, see find_work (which sees the lengths: where shares are short, they return at once)
+    const bool pieces = !int8 && rows * (c->capacity / (ch * W)) >= static_cast<int64_t>(kLongShare) * wave;
+    plan->ctas = pieces ? wave << kPiecesShift : plan->wave;
     plan->splits = c->capacity > 16 * min_team;
-    plan->workers = plan->ctas * (W / min_team);
+    plan->workers = plan->wave * (W / min_team) > plan->ctas ? plan->wave * (W / min_team) : plan->ctas;
     plan->jobs = static_cast<int>(rows < plan->workers ? rows : plan->workers);
     plan->join_bytes = (plan->jobs * sizeof(int4) + 255) / 256 * 256;
     plan->mz_bytes = (static_cast<size_t>(plan->workers) * 2 * 8 * plan->NB * sizeof(float2) + 255) / 256 * 256;
@@ -1042,7 +1082,7 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     if (e != cudaSuccess || !plan.splits) return static_cast<int>(e);
     // few rows: many parts each, a block of sixteen warps for a fragment; otherwise the parts of a row go at once, to the
     // warps of one block (64 rows of seven parts: 1.5 us so, 7 in large blocks, which an SM holds one of)
-    const bool few = prm.jobs_by_row && static_cast<int64_t>(plan.jobs) * kJoinAtOnce < plan.ctas;
+    const bool few = prm.jobs_by_row && static_cast<int64_t>(plan.jobs) * kJoinAtOnce < plan.wave;
     constexpr int kFew = 16, kMany = 4, F = (D / 16) * NB;
     cfg.gridDim = dim3(plan.jobs, few ? F : plan.jobs * (F / kMany) <= 5 * kSms ? F / kMany : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
     e = few ? cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kFew>, prm) : cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kMany>, prm);
@@ -1082,6 +1122,7 @@ int tilemix_paged_decode(const tilemix_paged_t* p, int32_t heads_q, float softma
     if ((rc = row_strides(q_stride, p->batch, heads_q, p->head_dim, false, prm.qs))) return rc;
     if ((rc = row_strides(out_stride, p->batch, heads_q, p->head_dim, true, prm.os))) return rc;
     if (workspace_bytes < plan.total) return TILEMIX_ERR_WORKSPACE;
+    prm.wave = plan.wave; prm.jobs = plan.jobs;
     prm.Hq = heads_q; prm.R = heads_q / p->heads_kv; prm.groups = plan.groups; prm.HG = plan.HG;
     prm.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(p->head_dim))) * kLog2e;
     prm.q = static_cast<const uint8_t*>(q);

@@ -99,9 +99,10 @@ class Setup:
         return out, present
 
 
-def attend(s, q, scale=0.0):
+def attend(s, q, scale=0.0, only=None):
     """float64 (out [B,Hq,d], lse [B,Hq]) and bounds of what the kernel may be off by, from the arithmetic it states.
 
+    ``only``: (sequence, head) pairs; the rest stays empty.
     u = half a step of the 16-bit type: outputs are rounded (u |o|).  A probability is a sum of two 16-bit numbers, the second
     the first's rounding error, rounded (u^2 of it; in all u^2 A, A = sum p |v|), over INT8 caches in FP16, and one FP16
     number where the outputs are BF16 (2^-11); those below 2^-28 of the largest are subnormal FP16 (at most 2^-39 of the
@@ -117,6 +118,8 @@ def attend(s, q, scale=0.0):
     tol, tol_lse = np.zeros((B, hq, d)), np.zeros((B, hq))
     qd = f64(q)
     for b in range(B):
+        if only is not None and not any(x == b for x, _ in only):
+            continue
         k, present = s.context("k", b)
         v, _ = s.context("v", b)
         k, v = k[present], v[present]
@@ -124,6 +127,8 @@ def attend(s, q, scale=0.0):
         if n == 0:
             continue
         for h in range(hq):
+            if only is not None and (b, h) not in only:
+                continue
             kk, vv = k[:, h * s.hk // hq], v[:, h * s.hk // hq]
             sc = (kk @ qd[b, h]) * scale
             top = sc.max()
@@ -138,13 +143,17 @@ def attend(s, q, scale=0.0):
     return out, lse, tol + torch.finfo(s.act).tiny * u, tol_lse
 
 
-def check_decode(s, q, res, scale=0.0):
-    out, lse, tol, tol_lse = attend(s, q, scale)
-    got = f64(res["out"])
+def check_decode(s, q, res, scale=0.0, only=None):
+    out, lse, tol, tol_lse = attend(s, q, scale, only)
+    got, lse_got = f64(res["out"]), res["lse"]
+    if only is not None:
+        b, h = (list(x) for x in zip(*only))
+        out, lse, tol, tol_lse, got = out[b, h], lse[b, h], tol[b, h], tol_lse[b, h], got[b, h]
+        lse_got = None if lse_got is None else lse_got[b, h]
     off = np.abs(got - out)
     assert (off <= tol).all(), f"out: {(off / tol).max():.2f} of the bound at {np.unravel_index((off / tol).argmax(), off.shape)}"
-    if res["lse"] is not None:
-        got = f64(res["lse"])
+    if lse_got is not None:
+        got = f64(lse_got)
         empty = np.isneginf(lse)
         assert (np.isneginf(got) == empty).all()
         assert (np.abs(got[~empty] - lse[~empty]) <= tol_lse[~empty]).all()

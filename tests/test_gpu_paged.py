@@ -206,6 +206,24 @@ def test_decode_many_rows(act, int8):
     ref.check_decode(s, q, tm().tilemix_paged_decode(s.cache(), q, want_lse=True))
 
 
+@pytest.mark.parametrize("act,int8,hk,lens", [("bf16", False, 8, [60000, 100, 0, 57100, 3]), ("fp16", False, 8, [1101] * 113), ("fp16", True, 4, [50000, 7, 41000])])
+def test_decode_large(act, int8, hk, lens):
+    """Shares long enough to be cut in pieces (16-bit caches), rows of many CTAs, more rows than there are workers; every row
+    finite, some of them against float64."""
+    s = ref.Setup(act, int8, 128, 64, hk, lens, seed=21, device=DEV)
+    q = query(s, 2 * hk, gain=2.0)
+    res = tm().tilemix_paged_decode(s.cache(), q, want_lse=True)
+    assert torch.isfinite(res["out"]).all() and torch.isfinite(res["lse"][torch.tensor(lens) > 0]).all()
+    ref.check_decode(s, q, res, only=[(b, h) for b in {0, 1, len(lens) // 2, len(lens) - 2, len(lens) - 1} for h in (0, hk, 2 * hk - 1)])
+    # any row that lost a part would differ from what the sequence gives by itself
+    for b in (0, len(lens) - 2):
+        one = tm().paged_cache(s.k_pool, s.v_pool, s.table[b:b + 1], s.cache_len[b:b + 1], s.k_scale, s.v_scale, dtype=s.act)
+        alone = tm().tilemix_paged_decode(one, q[b:b + 1], want_lse=True)
+        u = torch.finfo(s.act).eps
+        assert ((alone["out"][0].float() - res["out"][b].float()).abs() <= u * alone["out"][0].float().abs() + 2e-6).all()
+        assert (alone["lse"][0] - res["lse"][b]).abs().max() <= 1e-5 * alone["lse"][0].abs().max()
+
+
 @pytest.mark.parametrize("act,int8", KINDS)
 def test_decode_strides_and_scale(act, int8):
     s = ref.Setup(act, int8, 128, 32, 2, [100, 77], seed=4, nhd=True, device=DEV)
