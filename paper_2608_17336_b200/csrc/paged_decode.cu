@@ -3,16 +3,18 @@
 // HBM-bound: a cached (token, KV head) is 4 d bytes (16-bit cache) or 2 (d + 4) (INT8 codes and scales), read once, and serves
 // the R = H_q / H_k query heads of its group with 4 R d multiply-adds, far below the tensor cores' rate for R <= 16.  Hence
 // warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
-// at the cost of ~17 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.
+// at the cost of ~23 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.  16 x 32K keys of 128,
+// four KV heads, BF16: 160 us, 6.4 TB/s; 8 x 32K, eight KV heads, INT8: 93 us, 6.0 TB/s (read inside its loop 7.0); one
+// sequence of 500 keys 6.8 us, of which its steps' latencies are 4 and the joining kernel's 2.
 //
-// Layout of the work.  A warp owns a ring of three stages, starts its own copies and takes CHUNKS of 16 to 64 keys, which one
-// TMA box a page brings in, swizzled; no warp waits for another but at the end of a row.  Four or eight warps are a CTA, two
-// CTAs share an SM: 192 KB are on the way.  (A warp of its own for the copies of all could not start them fast
-// enough: four small ones a chunk, 8 x 32K keys of 128 in INT8 129 us, 101 so.)  Neighbouring chunks, one for each warp, are a UNIT; the units of all
-// (sequence, KV head) rows, one row behind the other, are dealt out to the CTAs in equal runs, so that a batch of unequal
-// lengths keeps every SM busy to the end.  A CTA finds its run from the lengths, which only the device knows.  Rows inside
-// its run it finishes itself; of a row that it shares with its neighbours it leaves a partial result (m, z, O) to the joining
-// kernel.  The copies run on across rows.
+// Layout of the work.  A warp owns a ring of stages, starts its own copies and takes CHUNKS of 16 to 64 keys, which one TMA box
+// a page brings in, swizzled; no warp waits for another but at the end of a row.  Four warps are a CTA, three CTAs share an SM
+// (two with more than eight query heads): 192 KB are on the way.  (A warp of its own for the copies of all could not start them
+// fast enough: four small ones a chunk, 8 x 32K keys of 128 in INT8 129 us, 101 so.)  Neighbouring chunks, one for each warp,
+// are a UNIT; the units of all (sequence, KV head) rows, one row behind the other, are dealt out to the CTAs in equal runs, so
+// that a batch of unequal lengths keeps every SM busy to the end.  A CTA finds its run from the lengths, which only the device
+// knows.  Rows inside its run it finishes itself; of a row that it shares with its neighbours it leaves a partial result
+// (m, z, O) to the joining kernel.  The copies run on across rows.
 //
 // Products.  S^T = K Q^T with the KEYS as the 16 rows of the MMA and eight query heads as its columns, then O^T = V^T P^T with
 // the head dimension as the rows: nothing of a 16-row operand is wasted on absent query heads, and O^T takes D / 32 * 8
@@ -585,12 +587,12 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
             auto attend = [&](auto blocks, auto part, int first_mb) {
                 constexpr int BLOCKS = decltype(blocks)::value;
                 constexpr bool PART = decltype(part)::value;
-                const uint32_t kst = ring_u32 + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128)), vst = kst + C::kVOff;
-                const uint8_t* const st = stages + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128));
+                [[maybe_unused]] const uint32_t kst = ring_u32 + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128)), vst = kst + C::kVOff;
+                [[maybe_unused]] const uint8_t* const st = stages + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128));
                 // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same).  A block alone sums its even and its
                 // odd steps apart: the chain of MMAs that wait for one another is half as long.
                 constexpr bool TWO = BLOCKS * NB == 1;
-                float sc[BLOCKS][NB][4], v_mul[BLOCKS][2], odd[BLOCKS][NB][4];
+                [[maybe_unused]] float sc[BLOCKS][NB][4], v_mul[BLOCKS][2], odd[BLOCKS][NB][4];
 #pragma unroll
                 for (int mb = 0; mb < BLOCKS; ++mb)
 #pragma unroll
@@ -627,12 +629,12 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                         }
                     }
                 }
-                const float* const sk = scale_ring + stage * (CH * 2) + 16 * first_mb + k_row;
+                [[maybe_unused]] const float* const sk = scale_ring + stage * (CH * 2) + 16 * first_mb + k_row;
 #pragma unroll
                 for (int mb = 0; mb < BLOCKS; ++mb)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float dk = 1.f;
+                        [[maybe_unused]] float dk = 1.f;
                         if constexpr (INT8) { dk = sk[16 * mb + 8 * i]; v_mul[mb][i] = sk[CH + 16 * mb + 8 * i]; }
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb)
@@ -730,7 +732,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 // ---- probabilities, and O^T += V^T P^T block by block
 #pragma unroll
                 for (int mb = 0; mb < BLOCKS; ++mb) {
-                    uint32_t p0[NB], p1[NB], r0[NB], r1[NB];
+                    [[maybe_unused]] uint32_t p0[NB], p1[NB], r0[NB], r1[NB];
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         float p[4];
@@ -1003,6 +1005,8 @@ int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* p
     if (rc) return rc;
     if (heads_q <= 0 || heads_q % p->heads_kv != 0) return TILEMIX_ERR_SHAPE;
     const int R = heads_q / p->heads_kv;
+    // Eight query heads of a KV head share a read of the cache, or sixteen (two rows of eight instead: 1 x 128K keys, sixteen
+    // heads 27.4 -> 31.5 us, 16 x 4K INT8 27.3 -> 32.6, BF16 37.0 -> 47.4).
     plan->NB = R > 8 ? 2 : 1;
     plan->groups = static_cast<int>(ceil_div(R, 8 * plan->NB));
     int W, ch, min_team, wave;
@@ -1118,7 +1122,7 @@ int tilemix_paged_decode(const tilemix_paged_t* p, int32_t heads_q, float softma
     int rc = resolve_decode(p, heads_q, &prm.c, &plan);
     if (rc) return rc;
     if (!q || !out || !workspace) return TILEMIX_ERR_NULL;
-    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return TILEMIX_ERR_ALIGN;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return TILEMIX_ERR_ALIGN;
     if ((rc = row_strides(q_stride, p->batch, heads_q, p->head_dim, false, prm.qs))) return rc;
     if ((rc = row_strides(out_stride, p->batch, heads_q, p->head_dim, true, prm.os))) return rc;
     if (workspace_bytes < plan.total) return TILEMIX_ERR_WORKSPACE;

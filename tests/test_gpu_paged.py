@@ -435,6 +435,28 @@ def test_decode_on_two_streams_at_once():
         assert all(torch.equal(x, want[i]) for x in got[i])
 
 
+def test_binding_refusals():
+    t = tm()
+    s = ref.Setup("fp16", True, 64, 16, 2, [20, 3], device=DEV)
+    c, q = s.cache(), query(s, 4)
+    x = torch.zeros((2, 2, 64), dtype=torch.float16, device=DEV)
+    bad = [lambda: t.tilemix_paged_decode(c, q.float()), lambda: t.tilemix_paged_decode(c, q[:1]), lambda: t.tilemix_paged_decode(c, q[..., :32]),
+           lambda: t.tilemix_paged_decode(c, q.cpu()), lambda: t.tilemix_paged_decode(c, q, out=q[:, :2]),
+           lambda: t.tilemix_paged_append(c, x, x.bfloat16()), lambda: t.tilemix_paged_append(c, x, x[:, :1]),
+           lambda: t.tilemix_paged_append(c, x, x, cu_new=torch.zeros(3, device=DEV)),
+           lambda: t.tilemix_paged_append(c, x, x, cu_new=torch.zeros(2, dtype=torch.int32, device=DEV)),
+           lambda: t.tilemix_paged_gather(c, x, x), lambda: t.tilemix_paged_gather(c, x, x, start=torch.zeros(2, device=DEV), cu_out=s.cache_len)]
+    for f in bad:
+        with pytest.raises((AssertionError, ValueError)):
+            f()
+    with pytest.raises(t.TilemixError):
+        t.tilemix_paged_append(c, x[:1], x[:1])                         # one token for two sequences, and no cu_new
+    with pytest.raises(t.TilemixError):
+        t.tilemix_paged_decode(c, torch.cat([q, q[:, :1]], 1))          # five query heads over two
+    with pytest.raises(t.TilemixError):
+        t.tilemix_paged_decode(c, q, workspace=torch.empty(64, dtype=torch.uint8, device=DEV))
+
+
 # ---------------------------------------------------------------------------------------------------- together
 
 @pytest.mark.parametrize("act,int8", KINDS)

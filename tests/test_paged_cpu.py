@@ -94,6 +94,9 @@ def test_refusals_of_the_calls(lib):
     assert decode(lib, ok, q=ctypes.c_void_p(4104)) == b.ERR_ALIGN and decode(lib, ok, out=ctypes.c_void_p(4100)) == b.ERR_ALIGN
     assert decode(lib, ok, qs=(I64 * 2)(8 * 128, 132)) == b.ERR_ALIGN and decode(lib, ok, os=(I64 * 2)(8 * 128, 64)) == b.ERR_SHAPE
     assert decode(lib, ok, nbytes=size - 1) == b.ERR_WORKSPACE
+    assert lib.tilemix_paged_decode(ctypes.byref(ok), 8, 0.0, ONE, None, ONE, None, ctypes.c_void_p(4098), ONE, size, None) == b.ERR_ALIGN
+    # more places than the counts have bits for
+    assert decode(lib, struct(max_pages=1 << 26, heads_kv=1024)) == b.ERR_SHAPE
 
 
 def test_binding_refuses_before_the_call():
