@@ -206,7 +206,8 @@ struct Work {
         return w;
     }
 };
-constexpr int kShortRow = 4;
+// (fewer than 1, 4, 8: 256 short INT8 sequences, heads of 64 26.5 / 25.0 / 25.0 us, 64 x 500 INT8, heads of 128 27.6 / 27.4 / 25.8)
+constexpr int kShortRow = 8;
 // SMs do not get the same share of the memory's bandwidth (equal shares of 8 x 32K keys end after 70 to 92 us, in the order of
 // their SMs' clusters).  Of long shares of a 16-bit cache the last eighth is a worker of its own, which goes to the SM that is
 // done first: blocks behind the first wave.  (us without and with: 64 ragged FP16 steps, heads of 64 97.4 / 92.8, 16 x 32K BF16
