@@ -83,11 +83,11 @@ struct Cfg {
     static constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
     static_assert(CH == 1 << kChShift, "chunks are whole boxes");
     static constexpr int MB = CH / 16;                              // blocks of 16 keys
-    // Blocks that a warp takes together, where a chunk has them whole: what does not depend on their number is done once for two,
-    // in twice the code and more registers.  (us together and one by one: 64 ragged FP16 steps, heads of 64 97 / 98, 16 x 8K
-    // INT8, heads of 64 32.6 / 36.6, 1 x 128K INT8, sixteen query heads 27.3 / 28.7; but 8 x 32K INT8, heads of 128 98.7 / 92.8,
-    // 64 x 500 29.3 / 27.6.)
-    static constexpr int kTogether = MB == 1 || (INT8 && NB == 1 && D == 128) ? 1 : 2;
+    // Blocks that a warp takes together, where a chunk has them whole: what does not depend on their number is done once for two.
+    // (us together and one by one: 64 ragged FP16 steps, heads of 64 97 / 98, 16 x 8K INT8, heads of 64 32.6 / 36.6, 1 x 128K INT8,
+    // sixteen query heads 27.3 / 28.7; 8 x 32K INT8, heads of 128 98 / 93 on a cool GPU, but 104 / 107 at the clock that the power
+    // cap leaves after half a second, where every instruction counts.)
+    static constexpr int kTogether = MB == 1 ? 1 : 2;
     static constexpr int kVOff = CH * D * kElt;                     // values behind the keys of a stage
     static constexpr int kBoxCols = INT8 ? 1 : D / 64;              // boxes side by side in a row of 16-bit values
     static constexpr int kScaleBytes = INT8 ? W * kStages * CH * 8 : 0;
@@ -101,10 +101,12 @@ struct Cfg {
     static constexpr float kUnOff = kHalfP ? 6.103515625e-5f : 1.f;
     static constexpr float kLine = kHalfP ? 1.5f : 8.f;
     // A probability goes to the tensor cores as two 16-bit numbers, what the first leaves out being the second, so that the
-    // error of an output is that of its own rounding (one number: 1.4 times that; an eighth more MMAs and a few conversions:
-    // 8 x 32K keys equal, 256 short INT8 sequences 24.8 -> 25.5 us, 32 x 4K INT8 ones 36 -> 39).  Not where FP16
-    // probabilities make BF16 outputs: one number has three bits more than the output.
-    static constexpr bool kTwoHalves = !(INT8 && std::is_same<T, __nv_bfloat16>::value);
+    // error of an output is that of its own rounding (one number: 1.4 times that).  Whole blocks of an INT8 cache: as one FP16
+    // number.  Two are an eighth more instructions there, under the power cap 7 % of 8 x 32K keys (97.7 / 104.5 us), of 32 x 4K
+    // 8 %, where a 16-bit cache, bound by its bytes, loses nothing.  The blocks at a row's end are two numbers all the same: a
+    // context of a few tokens, whose few errors do not average, is as exact as its values.
+    static constexpr bool kTwoHalves = !INT8;
+    static constexpr bool kTwoHalvesAtEnd = !(INT8 && std::is_same<T, __nv_bfloat16>::value);     // (FP16 has three bits more than the output)
     static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
 };
 constexpr float kNoMax = -1e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
@@ -338,7 +340,6 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     using C = Cfg<T, D, INT8, NB>;
     constexpr int CH = C::CH, MB = C::MB, W = C::W, kStages = C::kStages, kStageBytes = C::kStageBytes;
     constexpr bool BF16 = !C::kHalfP;
-    constexpr bool TWO_P = C::kTwoHalves;
     extern __shared__ uint8_t smem[];
     __shared__ __align__(8) uint64_t full_bar[W][kStages];
     __shared__ uint32_t hole_s[W][kStages];                          // bit 4 i: the 16 keys i of the chunk lie in a hole
@@ -588,6 +589,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
             auto attend = [&](auto blocks, auto part, int first_mb) {
                 constexpr int BLOCKS = decltype(blocks)::value;
                 constexpr bool PART = decltype(part)::value;
+                constexpr bool TWO_P = PART ? C::kTwoHalvesAtEnd : C::kTwoHalves;
                 [[maybe_unused]] const uint32_t kst = ring_u32 + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128)), vst = kst + C::kVOff;
                 [[maybe_unused]] const uint8_t* const st = stages + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128));
                 // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same).  A block alone sums its even and its
@@ -646,7 +648,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                             }
                     }
                 // ---- keys past the end and in holes do not exist, whatever lies in their rows
-                if (PART && (live < 16 * first_mb + 16 || holes != 0u)) {
+                if constexpr (PART) {
                     const bool hole = (holes >> (4 * first_mb)) & 1u;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {

@@ -104,8 +104,8 @@ def attend(s, q, scale=0.0, only=None):
 
     ``only``: (sequence, head) pairs; the rest stays empty.
     u = half a step of the 16-bit type: outputs are rounded (u |o|).  A probability is a sum of two 16-bit numbers, the second
-    the first's rounding error, rounded (u^2 of it; in all u^2 A, A = sum p |v|), over INT8 caches in FP16, and one FP16
-    number where the outputs are BF16 (2^-11); those below 2^-28 of the largest are subnormal FP16 (at most 2^-39 of the
+    the first's rounding error, rounded (u^2 of it; in all u^2 A, A = sum p |v|), over INT8 caches one FP16 number (2^-11;
+    of the last keys two); those below 2^-28 of the largest are subnormal FP16 (at most 2^-39 of the
     largest each).  A score of magnitude S (sum of |q_i k_i|,
     log2 units) is off by at most (d + 8) 2^-23 S (FP32 products summed in any order, each sum rounded to nearest or
     towards zero; scales), the exponential by 2^-22, FP32 sums over n keys by n 2^-24: relative errors of p of at most e,
@@ -113,7 +113,7 @@ def attend(s, q, scale=0.0, only=None):
     B, hq, d = q.shape
     scale = scale or 1 / math.sqrt(d)
     u = torch.finfo(s.act).eps / 2
-    up = 2.0 ** -11 if s.int8 and s.act == torch.bfloat16 else u * u
+    up = 2.0 ** -11 if s.int8 else u * u
     out, lse = np.zeros((B, hq, d)), np.full((B, hq), -np.inf)
     tol, tol_lse = np.zeros((B, hq, d)), np.zeros((B, hq))
     qd = f64(q)
