@@ -3,9 +3,9 @@
 // HBM-bound: a cached (token, KV head) is 4 d bytes (16-bit cache) or 2 (d + 4) (INT8 codes and scales), read once, and serves
 // the R = H_q / H_k query heads of its group with 4 R d multiply-adds, far below the tensor cores' rate for R <= 16.  Hence
 // warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
-// at the cost of ~23 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.  16 x 32K keys of 128,
-// four KV heads, BF16: 160 us, 6.4 TB/s; 8 x 32K, eight KV heads, INT8: 93 us, 6.0 TB/s (read inside its loop 7.0); one
-// sequence of 500 keys 6.8 us, of which its steps' latencies are 4 and the joining kernel's 2.
+// at the cost of ~21 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.  16 x 32K keys of 128,
+// four KV heads, BF16: 162 us, 6.3 TB/s; 8 x 32K, eight KV heads, INT8: 97 us, 5.7 TB/s, both under the power cap; one
+// sequence of 500 keys 6.6 us, of which the step's latencies are 4 and the joining kernel's 2.
 //
 // Layout of the work.  A warp owns a ring of stages, starts its own copies and takes CHUNKS of 16 to 64 keys, which one TMA box
 // a page brings in, swizzled; no warp waits for another but at the end of a row.  Four warps are a CTA, three CTAs share an SM
