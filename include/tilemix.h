@@ -351,7 +351,7 @@ int tilemix_decode_int8kv(const tilemix_decode_t* p, const void* q_f16, const vo
  *                        row); the value is x8 * delta.  A scale per token lets a token be written once: a scale per block
  *                        would have to requantise the open block with every token that joins it.
  * Both cache_len and block_table live on the device and are read by the kernels: a CUDA graph that holds these calls can be
- * replayed while the sequences grow.  A sequence's length is clamped to [0, max_pages * page_size].  A table entry outside
+ * replayed while the sequences grow.  Where a length is read from, it is clamped to [0, max_pages * page_size].  A table entry outside
  * [0, n_pages) is a hole (a page that is not resident): it is never accessed, and its keys are as if they did not exist.
  * Several sequences may share pages that are only read (a common prefix); a page that is appended to belongs to one. */
 #define TILEMIX_TYPE_FP16 0

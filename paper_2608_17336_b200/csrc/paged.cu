@@ -209,7 +209,8 @@ paged_append_kernel(const MoveParams prm) {
         const uint4* vf = reinterpret_cast<const uint4*>(prm.v + t * prm.v_st[2] + head * prm.v_st[1]) + part;
 #pragma unroll
         for (int p = 0; p < P; ++p) { k[p] = __ldcs(kf + p * LANES); v[p] = __ldcs(vf + p * LANES); }
-        const int pos = paged_len(c, b) - n_new + i;
+        const int64_t place = static_cast<int64_t>(c.cache_len[b]) - n_new + i;      // (not clamped: a token past the table has no place)
+        const int pos = place >= 0 && place < c.capacity ? static_cast<int>(place) : -1;
         if (pos >= 0) page = paged_page(c, b, pos);
         at = pos & ((1 << c.page_shift) - 1);
     }

@@ -107,18 +107,14 @@ def test_append_many_sequences():
 
 
 def test_append_drops_rows_without_a_place():
-    """More new rows than the length counts, lengths past the table, holes."""
-    s = ref.Setup("fp16", True, 128, 16, 2, [5, 40, 64, 30], device=DEV)
-    s.cache_len = torch.tensor([5, 1 << 28, -3, 30], dtype=torch.int32, device=DEV)     # clamped to the table's 64 tokens, to 0
+    """More new rows than the length counts, lengths at and past the table's end, negative ones, holes."""
+    s = ref.Setup("fp16", True, 128, 16, 2, [5, 40, 64, 30, 60, 64], device=DEV)
+    s.cache_len = torch.tensor([5, 1 << 30, -3, 30, 66, 64], dtype=torch.int32, device=DEV)       # the table has 64 places
     s.table[3, 0], s.table[3, 1] = -1, 1 << 30
-    s.cache_len.clamp_(-3, 1 << 28)
-    lens = s.cache_len.clone()
-    s.cache_len = lens.clamp(0, 64)
     g = torch.Generator().manual_seed(2)
-    x = torch.randn((2, 33, 2, 128), generator=g).half()
-    cu = np.array([0, 9, 16, 20, 33])
+    x = torch.randn((2, 43, 2, 128), generator=g).half()
+    cu = np.array([0, 9, 16, 20, 33, 38, 43])
     want = expected_append(s, x[0], x[1], cu)
-    s.cache_len = lens
     tm().tilemix_paged_append(s.cache(), x[0].to(DEV), x[1].to(DEV), torch.tensor(cu, dtype=torch.int32, device=DEV))
     for name, w in want.items():
         assert same_bits(getattr(s, name), w), name
