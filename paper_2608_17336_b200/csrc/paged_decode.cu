@@ -162,7 +162,7 @@ __device__ __forceinline__ uint32_t value_piece(int row, int piece) {
 // ---------------------------------------------------------------------------------------------------- the work list
 // Place in the list of units: rows (b, h) of n_units units, h = KV head * groups + group of query heads.
 struct Cursor {
-    int b, h, unit, n_units, len, left;      // left: units from here to the end of the worker's run
+    int b, h, unit, n_units, len, left;      // left: places from here to the end of the worker's run
 };
 __device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm, int unit_shift) {
     c.unit = 0;
@@ -179,7 +179,7 @@ __device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm
     }
 }
 
-// What a warp has to do.  A worker is a team of the CTA's warps: all of them, or, where there are rows enough for more workers
+// What a warp has to do: a run of places in the list of rows.  A worker is a team of the CTA's warps: all of them, or, where there are rows enough for more workers
 // and the rows are short (fewer than kShortRow chunks a warp of the team on average), half of them.  Chunks are CH keys, or
 // fewer where there would be fewer units than CTAs.  A unit is a chunk for each warp of the team; the U units go to n workers in
 // shares of U / n or one more (and a long share to two workers, see below).
@@ -188,6 +188,7 @@ struct Work {
     int team_shift, chunk_shift, worker;
     int base, longer;                        // units of a share; the first `longer` shares have one more
     int pieces_shift, small;                 // pieces of a share: the first, and others of `small` units
+    int extra;                               // units that a row counts as beyond its own, behind them
 
     __device__ __forceinline__ int share_first(int i) const { return i * base + min(i, longer); }
     __device__ __forceinline__ int units_of(int w) const {
@@ -216,6 +217,11 @@ constexpr int kShortRow = 8;
 // 161.2 / 159.7; a block's entry costs as much as that gains where shares are short, 16 x 4K BF16, sixteen query heads
 // 37.1 / 42.9, and in the INT8 form, 8 x 32K 93.2 / 97.0.)
 constexpr int kPiecesShift = 1, kLongShare = 32;
+// The start of a row and its merge cost a worker as much as some blocks of 16 keys; unless shares are short, a row counts as
+// that many more, or the workers with the most rows end last.  (us with 0, 2, 4, 6 blocks: 64 x 500 BF16 35.4 / 32.0 / 31.9 /
+// 31.9, 200 x 300 BF16, heads of 64 22.7 / 19.5 / 19.2 / 19.4, 256 short INT8, heads of 64 24.5 / 24.5 / 23.3 / 23.3, 32 x 4K
+// INT8 37.2 / 36.8 / 36.8 / 37.7.)
+constexpr int kRowBlocks = 4;
 template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE, bool PIECES>
 __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     constexpr int kTeamShift = W == 8 ? 3 : 2, kMinShift = MIN_TEAM == 2 ? 1 : 2;
@@ -243,7 +249,12 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
         --w.team_shift;
     const int unit_shift = w.chunk_shift + w.team_shift;
     auto units_of = [&](int len) { return (len + (1 << unit_shift) - 1) >> unit_shift; };
-    const int U = __reduce_add_sync(0xffffffffu, sum_of(units_of)) * prm.HG, n = min(ctas << (kTeamShift - w.team_shift), U);
+    int U = __reduce_add_sync(0xffffffffu, sum_of(units_of)) * prm.HG;
+    const int most = ctas << (kTeamShift - w.team_shift), n = min(most, U), extra = kRowBlocks << 4 >> w.chunk_shift;
+    if (U > 2 * extra * most) {
+        w.extra = extra;
+        U += extra * rows;
+    }
     if (n > 0) { w.base = U / n; w.longer = U - w.base * n; }
     const int block = blockIdx.x;
     if (PIECES && gridDim.x > ctas && w.team_shift == kTeamShift && w.base >= kLongShare) {
@@ -257,9 +268,9 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     }
     Cursor& c = w.at;
     const int first = w.first_of(w.worker);
-    int before = 0;                          // units of the sequences before the 32 in hand
+    int before = 0;                          // places of the sequences before the 32 in hand
     auto among = [&](int b0, int len) -> bool {
-        const int mine = units_of(len), all = __reduce_add_sync(0xffffffffu, mine) * prm.HG;
+        const int mine = len > 0 ? units_of(len) + w.extra : 0, all = __reduce_add_sync(0xffffffffu, mine) * prm.HG;
         if (before + all <= first) {
             before += all;
             return false;
@@ -272,11 +283,12 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
         }
         const int l = __ffs(__ballot_sync(0xffffffffu, before + upto > first)) - 1;
         c.b = b0 + l;
-        c.n_units = __shfl_sync(0xffffffffu, mine, l);
+        const int places = __shfl_sync(0xffffffffu, mine, l);
+        c.n_units = places - w.extra;
         c.len = __shfl_sync(0xffffffffu, len, l);
-        const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - c.n_units * prm.HG);
-        c.h = at / c.n_units;
-        c.unit = at - c.h * c.n_units;
+        const int at = first - before - (__shfl_sync(0xffffffffu, upto, l) - places * prm.HG);
+        c.h = at / places;
+        c.unit = at - c.h * places;
         c.left = w.units_of(w.worker);
         return true;
     };
@@ -413,7 +425,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
         const int u_end = min(ic.n_units, ic.unit + ic.left);
         next_start = (ic.unit << unit_shift) + (member << chunk_shift);
         next_end = min(ic.len, u_end << unit_shift);
-        ic.left -= u_end - ic.unit;
+        ic.left -= u_end - ic.unit + work.extra;
         next_hk = prm.groups == 1 ? ic.h : ic.h / prm.groups;
         next_table = c.table + ic.b * c.table_stride;
         if constexpr (INT8) next_scale = (lane < kQuads ? c.k_scale : c.v_scale) + (static_cast<int64_t>(next_hk) << c.page_shift);
@@ -482,12 +494,12 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     if (member == 0 && lane == 0) {
         const int worker = work.worker;
         int4 job = make_int4(-1, 0, 0, 0);
-        if (cc.left > 0 && cc.unit > 0) {
+        if (cc.left > 0 && cc.unit > 0 && cc.unit < cc.n_units) {
             const int row_first = work.first_of(worker) - cc.unit, before = work.first_of(worker - 1);
             if (before <= row_first) {
                 const int last = work.worker_of(row_first + cc.n_units - 1);
                 // row, the slot of the part in front, and the workers whose first slots hold the others
-                job = make_int4(cc.b * prm.HG + cc.h, 2 * (worker - 1) + (before == row_first ? 0 : 1), worker, last - worker + 1);
+                job = make_int4(cc.b * prm.HG + cc.h, 2 * (worker - 1) + (before >= row_first - work.extra ? 0 : 1), worker, last - worker + 1);
             }
         }
         // (by worker: a job each; teams that there are not, and blocks without work, write theirs too)
@@ -817,15 +829,16 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 
         // ------------------------------------------------ the warps' results of the segment, merged in the stages read last
         // (every warp holds the same places of O^T; a warp without a chunk here has no stage to itself: its place is not read)
-        const bool whole = cc.unit == 0 && u_end == cc.n_units;
+        const bool none = cc.unit >= cc.n_units, whole = cc.unit == 0 && u_end == cc.n_units;
         const int slot = 2 * work.worker + (first_segment ? 0 : 1), b = cc.b, h = cc.h;
         if (whole && prm.jobs_by_row && member == 0 && lane == 0) prm.join[b * prm.HG + h] = make_int4(-1, 0, 0, 0);
-        first_segment = false;
-        cc.left -= u_end - cc.unit;
+        first_segment = first_segment && none;
+        cc.left -= u_end - cc.unit + work.extra;
         if (cc.left > 0) {
             next_row(cc, prm, unit_shift);
             if (cc.left > 0) fetch_q(cc);                     // (on the way during the merge)
         }
+        if (none) continue;                                   // (a run that begins behind the units of a row)
         float4* mine = reinterpret_cast<float4*>(ring + (warp * kStages + held) * kStageBytes);
         if (lane == 0) {
             v_ref_s[warp] = any && !failed ? (INT8 ? v_ref : 1.f) : -1.f;
@@ -912,9 +925,9 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 // Joins the parts of the rows that several workers shared.  A job (row, s, w, n) names slot s and the first slots of n workers
 // from w on.  (A kernel of its own, whose launch overlaps the step: the last CTA of a row joining it at its end, found by a
 // counter or by words that the others set, waits for fences and atomics longer than a grid does for its predecessor: one
-// sequence of 500 keys 6.6 us so, 11.0 and 9.0 that way, 8 x 32 K 98, 104, 104.)  What bounds it is the round trips: the parts are loaded kJoinAtOnce at a time.  A row of up to that many has a
-// warp for every fragment; the parts of others are shared out over the warps, fragment by fragment (by a block each where rows
-// are few).
+// sequence of 500 keys 6.6 us so, 11.0 and 9.0 that way, 8 x 32 K 98, 104, 104.)  What bounds it is the round trips: the parts
+// are loaded kJoinAtOnce at a time.  A row of up to twice as many has a warp for every fragment; the parts of others are shared
+// out over the warps, fragment by fragment (by a block each where rows are few).
 constexpr int kJoinAtOnce = 8;
 struct Part {
     float4 o, mz;                   // sums; maximum and sum of column 2 t, of column 2 t + 1

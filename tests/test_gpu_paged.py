@@ -202,6 +202,16 @@ def test_decode_many_rows(act, int8):
     ref.check_decode(s, q, tm().tilemix_paged_decode(s.cache(), q, want_lse=True))
 
 
+@pytest.mark.parametrize("act,int8,d", [("bf16", False, 128), ("fp16", False, 64), ("fp16", True, 128), ("bf16", True, 64)])
+def test_decode_many_short_rows(act, int8, d):
+    """Runs of several short rows a worker, of very different lengths, which begin and end anywhere in and between rows; empty
+    sequences between them and at the end."""
+    lens = [0 if i % 7 == 3 else 1 + (i * i * 131 + 77 * i) % 800 for i in range(140)] + [1, 1, 0]
+    s = ref.Setup(act, int8, d, 16, 8, lens, seed=31, stale=float("nan"), device=DEV)
+    q = query(s, 8, gain=2.0)
+    ref.check_decode(s, q, tm().tilemix_paged_decode(s.cache(), q, want_lse=True))
+
+
 @pytest.mark.parametrize("act,int8,hk,lens", [("bf16", False, 8, [60000, 100, 0, 57100, 3]), ("fp16", False, 8, [1101] * 113), ("fp16", True, 4, [50000, 7, 41000])])
 def test_decode_large(act, int8, hk, lens):
     """Shares long enough to be cut in pieces (16-bit caches), rows of many CTAs, more rows than there are workers; every row
