@@ -499,9 +499,12 @@ def paged_cache(k_pool, v_pool, block_table, cache_len, k_scale=None, v_scale=No
         dtype = torch.float16 if int8 else k_pool.dtype
     assert dtype in _ACT and k_pool.dtype in (dtype, torch.int8) and v_pool.dtype == k_pool.dtype
     assert k_pool.dim() == 4 and v_pool.shape == k_pool.shape and k_pool.stride(3) == 1 and v_pool.stride(3) == 1
+    # (strides of zero mean dense ones in the struct)
+    assert k_pool.stride(2) > 0 and v_pool.stride(2) > 0, "the pools are memory of their own, not expanded views"
     n_pages, hk, page_size, d = k_pool.shape
     assert block_table.dtype == torch.int32 and block_table.dim() == 2 and (block_table.stride(1) == 1 or block_table.shape[1] <= 1)
     B, max_pages = block_table.shape
+    assert B <= 1 or block_table.stride(0) >= max(max_pages, 1), "rows of block_table overlap (an expanded view?)"
     assert cache_len.dtype == torch.int32 and cache_len.shape == (B,) and cache_len.is_contiguous()
     held = [k_pool, v_pool, block_table, cache_len]
     if int8:

@@ -153,3 +153,17 @@ def test_one_fma_codes_hold_for_bfloat16():
                 # x r + 1.5 2^23, rounded once to the nearest integer, ties to even: x (8 bits) r (24 bits) is exact
                 got = np.rint(x.astype(np.float64) * np.float64(r))
             assert np.array_equal(got, want), (e, a)
+
+
+def test_expanded_views_are_refused():
+    """Strides of zero would mean dense ones: an expanded table or pool must not be read past its end."""
+    pool, n = torch.zeros((4, 2, 16, 64), dtype=torch.float16), torch.zeros(3, dtype=torch.int32)
+    table = torch.zeros((3, 2), dtype=torch.int32)
+    with pytest.raises(AssertionError, match="overlap"):
+        b.paged_cache(pool, pool, table[:1].expand(3, 2), n)
+    with pytest.raises(AssertionError, match="expanded"):
+        b.paged_cache(pool, torch.zeros(64, dtype=torch.float16).expand(4, 2, 16, 64), table, n)
+    with pytest.raises(AssertionError, match="one CUDA device"):        # (the others pass the checks of shapes and strides)
+        b.paged_cache(pool, pool, table, n)
+    with pytest.raises(AssertionError, match="one CUDA device"):
+        b.paged_cache(pool, pool, table[:1], n[:1])
