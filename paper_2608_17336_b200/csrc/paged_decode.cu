@@ -5,7 +5,7 @@
 // warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
 // at the cost of ~21 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.  16 x 32K keys of 128,
 // four KV heads, BF16: 162 us, 6.3 TB/s; 8 x 32K, eight KV heads, INT8: 97 us, 5.7 TB/s, both under the power cap; one
-// sequence of 500 keys 6.6 us, of which the step's latencies are 4 and the joining kernel's 2.
+// sequence of 500 keys 6.8 us, of which the step's latencies are 4 and the joining kernel's 2.
 //
 // Layout of the work.  A warp owns a ring of stages, starts its own copies and takes CHUNKS of 16 to 64 keys, which one TMA box
 // a page brings in, swizzled; no warp waits for another but at the end of a row.  Four warps are a CTA, three CTAs share an SM
@@ -209,7 +209,8 @@ struct Work {
         return w;
     }
 };
-// (fewer than 1, 4, 8: 256 short INT8 sequences, heads of 64 26.5 / 25.0 / 25.0 us, 64 x 500 INT8, heads of 128 27.6 / 27.4 / 25.8)
+// (fewer than 4, 8, 16: 64 x 500 BF16 31.7 / 32.0 / 33.0 us, 32 x 2K INT8, one query head a KV head, heads of 64
+// 25.9 / 25.0 / 25.2)
 constexpr int kShortRow = 8;
 // SMs do not get the same share of the memory's bandwidth (equal shares of 8 x 32K keys end after 70 to 92 us, in the order of
 // their SMs' clusters).  Of long shares of a 16-bit cache the last eighth is a worker of its own, which goes to the SM that is
