@@ -100,6 +100,8 @@ struct Cfg {
     static constexpr float kOff = kHalfP ? 14.f : 0.f;
     static constexpr float kUnOff = kHalfP ? 6.103515625e-5f : 1.f;
     static constexpr float kLine = kHalfP ? 1.5f : 8.f;
+    // bfloat16 queries over INT8 codes are multiplied by a power of two of their row (see the segment's start)
+    static constexpr bool kScaledQ = INT8 && std::is_same<T, __nv_bfloat16>::value;
     // A probability goes to the tensor cores as two 16-bit numbers, what the first leaves out being the second, so that the
     // error of an output is that of its own rounding (one number: 1.4 times that).  Whole blocks of an INT8 cache: as one FP16
     // number.  Two are an eighth more instructions there, under the power cap 7 % of 8 x 32K keys (97.7 / 104.5 us), of 32 x 4K
@@ -109,7 +111,12 @@ struct Cfg {
     static constexpr bool kTwoHalvesAtEnd = !(INT8 && std::is_same<T, __nv_bfloat16>::value);     // (FP16 has three bits more than the output)
     static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
 };
-constexpr float kNoMax = -1e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
+constexpr float kNoMax = -3.4028234663852886e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
+// Scores are FP32 numbers, log2 units, once they are scaled; what is exponentiated is their difference to a whole number.  Up to
+// this size a whole number and kOff add up exactly; from here on the maximum is a whole number by itself and kOff is left out,
+// so that the exponent of the largest key is 0 whatever the scores' size (kOff less a maximum above 2^25 is rounded, by 2 and more:
+// a probability beyond FP16's range, or none at all).
+constexpr float kExact = 8388608.f;     // 2^23
 
 // ---------------------------------------------------------------------------------------------------- warp-level pieces
 template <bool BF16>
@@ -543,11 +550,10 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     while (cc.left > 0) {
         // ------------------------------------------------ a row, or this worker's part of it
         const int u_end = min(cc.n_units, cc.unit + cc.left);
-        float q_mul[NB][2];                                   // what a score is multiplied by
+        [[maybe_unused]] float q_mul[NB][2];                  // what a score is multiplied by yet: a power of two
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            q_mul[nb][0] = q_mul[nb][1] = prm.scale_log2;
-            if constexpr (INT8 && std::is_same<T, __nv_bfloat16>::value) {
+            if constexpr (C::kScaledQ) {
                 // bfloat16 queries as FP16: multiplied by the power of two that brings the row's largest value to
                 // [2^13, 2^14); eight mantissa bits fit, and what becomes subnormal is below 2^-27 of the largest
                 uint32_t top = 0u;
@@ -569,8 +575,8 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                         const float2 f = act_to_float2(qf[nb][i][k], __nv_bfloat16());
                         qf[nb][i][k] = act_pack2(f.x * up, f.y * up, __half());
                     }
-                q_mul[nb][0] *= __shfl_sync(0xffffffffu, down, 8 * t);
-                q_mul[nb][1] *= __shfl_sync(0xffffffffu, down, 8 * t + 4);
+                q_mul[nb][0] = __shfl_sync(0xffffffffu, down, 8 * t);
+                q_mul[nb][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
             }
         }
 
@@ -650,14 +656,17 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 for (int mb = 0; mb < BLOCKS; ++mb)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        [[maybe_unused]] float dk = 1.f;
-                        if constexpr (INT8) { dk = sk[16 * mb + 8 * i]; v_mul[mb][i] = sk[CH + 16 * mb + 8 * i]; }
+                        // (the scale is part of the score before the maximum is taken: equal keys have equal scores, and the
+                        // largest one's exponent is what the maximum says.  As a factor of the exponent's multiply-add, its
+                        // rounding would be a difference between the two, as large as the scores.)
+                        float mul = prm.scale_log2;
+                        if constexpr (INT8) { mul *= sk[16 * mb + 8 * i]; v_mul[mb][i] = sk[CH + 16 * mb + 8 * i]; }
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
                                 if constexpr (TWO) sc[mb][nb][2 * i + k] += odd[mb][nb][2 * i + k];
-                                if constexpr (INT8) sc[mb][nb][2 * i + k] *= dk;
+                                sc[mb][nb][2 * i + k] *= mul;
                             }
                     }
                 // ---- keys past the end and in holes do not exist, whatever lies in their rows
@@ -691,7 +700,10 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]);
+                            for (int k = 0; k < 4; ++k) {
+                                if constexpr (C::kScaledQ) e[mb][nb][k] = fmaf(sc[mb][nb][k], q_mul[nb][k & 1], sub[nb][k & 1]);
+                                else e[mb][nb][k] = sc[mb][nb][k] + sub[nb][k & 1];
+                            }
                 };
                 exponents();
 #pragma unroll
@@ -717,7 +729,9 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                            const float s_new = fminf(sub[nb][k], C::kOff - ceilf(x * q_mul[nb][k]));
+                            if constexpr (C::kScaledQ) x *= q_mul[nb][k];
+                            x = ceilf(x);
+                            const float s_new = fminf(sub[nb][k], (fabsf(x) < kExact ? C::kOff : 0.f) - x);
                             alpha[nb][k] = fast_exp2(s_new - sub[nb][k]);
                             sub[nb][k] = s_new;
                             z[nb][k] *= alpha[nb][k];
