@@ -402,9 +402,9 @@ int tilemix_paged_gather(const tilemix_paged_t* c, const int32_t* start, const i
 
 /* One new query token per sequence attends to the first cache_len[b] tokens of the cache:
  *   s_j = scale * (q . k_j),  o = sum_j softmax(s)_j v_j,  lse = ln sum_j exp(s_j),
- * with the values that the cache stands for; queries are not quantised.  FP32 scores, statistics and sums; for
- * the product with V a probability is the sum of two 16-bit numbers; over an INT8 cache one FP16 number, but (FP16
- * outputs) for the last keys of a row.
+ * with the values that the cache stands for; queries are not quantised.  FP32 scores, statistics and sums; for the product
+ * with V a probability is the sum of two 16-bit numbers, over an INT8 cache with BF16 outputs one FP16 number (three bits more
+ * than the output has).
  *   heads_q   any multiple of heads_kv
  *   softmax_scale  <= 0 means 1/sqrt(head_dim)
  *   q, out    [batch, Hq, d] in act_type; strides in elements for (batch, head), NULL = dense; 16-byte multiples

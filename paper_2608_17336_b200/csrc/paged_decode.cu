@@ -103,12 +103,12 @@ struct Cfg {
     // bfloat16 queries over INT8 codes are multiplied by a power of two of their row (see the segment's start)
     static constexpr bool kScaledQ = INT8 && std::is_same<T, __nv_bfloat16>::value;
     // A probability goes to the tensor cores as two 16-bit numbers, what the first leaves out being the second, so that the
-    // error of an output is that of its own rounding (one number: 1.4 times that).  Whole blocks of an INT8 cache: as one FP16
-    // number.  Two are an eighth more instructions there, under the power cap 7 % of 8 x 32K keys (97.7 / 104.5 us), of 32 x 4K
-    // 8 %, where a 16-bit cache, bound by its bytes, loses nothing.  The blocks at a row's end are two numbers all the same: a
-    // context of a few tokens, whose few errors do not average, is as exact as its values.
-    static constexpr bool kTwoHalves = !INT8;
-    static constexpr bool kTwoHalvesAtEnd = !(INT8 && std::is_same<T, __nv_bfloat16>::value);     // (FP16 has three bits more than the output)
+    // error of an output is that of its own rounding (one number: 1.4 times that).  Every key's does, so that what a row is
+    // rounded by does not depend on the rows beside it, which have a say in how chunks are cut.  bfloat16 outputs over an INT8
+    // cache: one FP16 number, which has three bits more than the output.  (us, two numbers and one: 8 x 32K INT8
+    // 97.9 / 97.6, at the clock that the power cap leaves 102.6 / 95.5, 32 x 4K 39.2 / 36.8, 64 x 500 26.7 / 25.0, 256 short, heads of
+    // 64 24.2 / 23.4.)
+    static constexpr bool kTwoHalves = !kScaledQ;
     static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
 };
 constexpr float kNoMax = -3.4028234663852886e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
@@ -608,7 +608,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
             auto attend = [&](auto blocks, auto part, int first_mb) {
                 constexpr int BLOCKS = decltype(blocks)::value;
                 constexpr bool PART = decltype(part)::value;
-                constexpr bool TWO_P = PART ? C::kTwoHalvesAtEnd : C::kTwoHalves;
+                constexpr bool TWO_P = C::kTwoHalves;
                 [[maybe_unused]] const uint32_t kst = ring_u32 + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128)), vst = kst + C::kVOff;
                 [[maybe_unused]] const uint8_t* const st = stages + stage * kStageBytes + first_mb * (16 * (INT8 ? D : 128));
                 // ---- S^T: sc[mb][nb] = (row g, columns 2 t, 2 t + 1), (row g + 8, the same).  A block alone sums its even and its
