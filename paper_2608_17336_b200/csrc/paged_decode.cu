@@ -480,14 +480,15 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
         next_start += unit_keys;
         prepare();
     };
-    // Bounded wait for the chunk in `stage`.
+    // Bounded wait for the chunk in `stage`; the verdict is the warp's (a copy may land for some lanes as others give up, and
+    // what follows takes the whole warp).
     auto landed = [&](int stage, uint32_t phase) -> bool {
         const uint32_t bar = ptx::smem_u32(&full_bar[warp][stage]);
-        if (ptx::mbar_try_wait(bar, phase)) return true;
+        if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, phase))) return true;
         const uint64_t begin = ptx::globaltimer_ns();
         uint32_t spins = 0;
-        while (!ptx::mbar_try_wait(bar, phase))
-            if ((++spins & 63u) == 0u && ptx::globaltimer_ns() - begin > prm.wait_limit_ns) return false;
+        while (!__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, phase)))
+            if ((++spins & 63u) == 0u && __any_sync(0xffffffffu, ptx::globaltimer_ns() - begin > prm.wait_limit_ns)) return false;
         return true;
     };
     if (ic.left > 0) {
