@@ -351,7 +351,9 @@ int tilemix_decode_int8kv(const tilemix_decode_t* p, const void* q_f16, const vo
  *                        row); the value is x8 * delta.  A scale per token lets a token be written once: a scale per block
  *                        would have to requantise the open block with every token that joins it.
  * Both cache_len and block_table live on the device and are read by the kernels: a CUDA graph that holds these calls can be
- * replayed while the sequences grow.  Where a length is read from, it is clamped to [0, max_pages * page_size].  A table entry outside
+ * replayed while the sequences grow.  Neither may change while a call runs that was given them (change them on the call's
+ * stream): such a call ends, and stays inside its buffers, but what it writes to its outputs (append: to the pages that the
+ * table names) is not defined.  Where a length is read from, it is clamped to [0, max_pages * page_size].  A table entry outside
  * [0, n_pages) is a hole (a page that is not resident): it is never accessed, and its keys are as if they did not exist.
  * Several sequences may share pages that are only read (a common prefix); a page that is appended to belongs to one. */
 #define TILEMIX_TYPE_FP16 0
@@ -453,6 +455,9 @@ int tilemix_tensor_peak_probe(int int8, int n_mma, int* n_ctas, void* workspace,
  *              status record, every warp leaves out its second chunk of keys, and the rows concerned become NaN
  *   which = 3  the streaming quantiser's producer leaves out the second block of every CTA; the quantiser has no
  *              status record: a CTA that gives up writes NaN into the scales of the blocks it did not finish
+ *   which = 4 to 7  in tilemix_paged_decode the lengths are not what they are, as if they had changed between two reads: every
+ *              second warp takes them for 16 (4) or 4096 (5) tokens shorter, every warp's copies those after its first row for
+ *              4096 longer (6) or shorter (7); warps wait for what nobody does and give up, and the outputs are not defined
  *   which = 0  normal operation, limit back to the default of 2 s (wait_limit_ns is ignored)
  * Returns TILEMIX_OK or TILEMIX_ERR_SHAPE. */
 int tilemix_test_drop_copy(int which, uint64_t wait_limit_ns);

@@ -44,7 +44,7 @@ constexpr int kSms = 148;
 struct PagedDecodeParams {
     PagedCache c;
     int Hq, R;                      // query heads, query heads per KV head
-    int wave, jobs;                 // CTAs that run at the same time; jobs of the joining kernel
+    int wave, jobs, workers;        // CTAs that run at the same time; jobs of the joining kernel; workers that there may be
     int groups, HG;                 // groups of up to 8 NB query heads per KV head; rows of a sequence (Hk * groups)
     float scale_log2;
     const uint8_t* q;
@@ -57,7 +57,16 @@ struct PagedDecodeParams {
     float2* part_mz;                // [2 workers][8 NB]: maximum (log2 domain) and sum
     unsigned long long wait_limit_ns;
     int drop_chunk;                 // testing aid: every warp leaves out the copies of its chunk of this number (-1: none)
+    int skew, skew_copies;          // testing aid: odd warps take every length for that much shorter; the copies, later rows' for that much longer
 };
+
+// Length of sequence b.  Every warp reads the lengths for itself, some of them twice; one that changes while the call runs can
+// leave the warps of a CTA, or a warp's copies and its products, with different ideas of what there is to do.  Hence every wait
+// for another warp is bounded as those for copies are, what one warp hands to another is in bounds whatever it holds, and no
+// CTA ends with copies on the way.
+__device__ __forceinline__ int length_of(const PagedDecodeParams& prm, int b) {
+    return max(paged_len(prm.c, b) - ((threadIdx.x & 32) != 0 ? prm.skew : 0), 0);
+}
 
 // The pools as tensor maps: boxes of a chunk, or of a page if that is smaller, and boxes of 16 tokens for smaller chunks.
 struct PoolMaps {
@@ -171,7 +180,7 @@ __device__ __forceinline__ uint32_t value_piece(int row, int piece) {
 struct Cursor {
     int b, h, unit, n_units, len, left;      // left: places from here to the end of the worker's run
 };
-__device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm, int unit_shift) {
+__device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm, int unit_shift, int longer) {
     c.unit = 0;
     if (++c.h == prm.HG) {
         c.h = 0;
@@ -180,7 +189,7 @@ __device__ __forceinline__ void next_row(Cursor& c, const PagedDecodeParams& prm
                 c.left = 0;
                 return;
             }
-            c.len = paged_len(prm.c, c.b);
+            c.len = min(max(__shfl_sync(0xffffffffu, length_of(prm, c.b), 0) + longer, 0), prm.c.capacity);
             c.n_units = (c.len + (1 << unit_shift) - 1) >> unit_shift;
         } while (c.n_units == 0);
     }
@@ -238,13 +247,13 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     constexpr int kKept = 8;
     int kept[kKept];
 #pragma unroll
-    for (int i = 0; i < kKept; ++i) kept[i] = lane + 32 * i < B ? paged_len(prm.c, lane + 32 * i) : 0;
+    for (int i = 0; i < kKept; ++i) kept[i] = lane + 32 * i < B ? length_of(prm, lane + 32 * i) : 0;
     // sum of f(length) over the sequences, of this lane
     auto sum_of = [&](auto f) {
         int sum = 0;
 #pragma unroll
         for (int i = 0; i < kKept; ++i) sum += f(kept[i]);
-        for (int b = 32 * kKept + lane; b < B; b += 32) sum += f(paged_len(prm.c, b));
+        for (int b = 32 * kKept + lane; b < B; b += 32) sum += f(length_of(prm, b));
         return sum;
     };
     const int blocks = __reduce_add_sync(0xffffffffu, sum_of([](int len) { return (len + 15) >> 4; })) * prm.HG;     // of 16 keys
@@ -304,7 +313,7 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     for (int i = 0; i < kKept; ++i)
         if (32 * i < B && among(32 * i, kept[i])) return w;
     for (int b0 = 32 * kKept; b0 < B; b0 += 32)
-        if (among(b0, b0 + lane < B ? paged_len(prm.c, b0 + lane) : 0)) return w;
+        if (among(b0, b0 + lane < B ? length_of(prm, b0 + lane) : 0)) return w;
     return w;
 }
 
@@ -361,7 +370,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     constexpr int CH = C::CH, MB = C::MB, W = C::W, kStages = C::kStages, kStageBytes = C::kStageBytes;
     constexpr bool BF16 = !C::kHalfP;
     extern __shared__ uint8_t smem[];
-    __shared__ __align__(8) uint64_t full_bar[W][kStages];
+    __shared__ __align__(8) uint64_t full_bar[W][kStages], team_bar[1 + W / C::kMinTeam];     // team_bar[0]: of all warps
     __shared__ uint32_t hole_s[W][kStages];                          // bit 4 i: the 16 keys i of the chunk lie in a hole
     __shared__ __align__(8) float m_s[W][8 * NB], z_s[W][8 * NB];
     __shared__ float v_ref_s[W];
@@ -371,11 +380,15 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     const PagedCache& c = prm.c;
 
     if (lane == 0) {
+        held_s[warp] = 0;                    // (read by the other warps of a team, should a wait for this one run out)
+        v_ref_s[warp] = -1.f;
+        if (warp == 0)
+            for (int i = 0; i < 1 + W / C::kMinTeam; ++i) ptx::mbar_init(ptx::smem_u32(&team_bar[i]), i == 0 ? W : C::kMinTeam);
         // (arrivals: the lane that announces the bytes of the boxes, and every lane with its part of the scales)
         for (int i = 0; i < kStages; ++i) ptx::mbar_init(ptx::smem_u32(&full_bar[warp][i]), INT8 ? 33 : 1);
         ptx::fence_mbar_init();
     }
-    __syncwarp();
+    __syncthreads();
     ptx::griddep_wait();                     // the cache, the lengths and the queries may be the work of the kernel before
     ptx::griddep_launch_dependents();
 
@@ -383,7 +396,28 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     const int team = 1 << work.team_shift, member = warp & (team - 1), team_no = warp >> work.team_shift;
     const int chunk_shift = work.chunk_shift, chunk = 1 << chunk_shift, unit_shift = chunk_shift + work.team_shift, unit_keys = 1 << unit_shift;
     Cursor cc = work.at;
-    auto team_sync = [&]() { ptx::bar_sync_named(1 + team_no, 32 * team); };
+
+    // Bounded wait; the verdict is the warp's (a copy may land for some lanes as others give up, and what follows takes the whole
+    // warp).
+    auto passed = [&](uint32_t bar, uint32_t phase, uint64_t limit_ns) -> bool {
+        if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, phase))) return true;
+        const uint64_t begin = ptx::globaltimer_ns();
+        uint32_t spins = 0;
+        while (!__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, phase)))
+            if ((++spins & 63u) == 0u && __any_sync(0xffffffffu, ptx::globaltimer_ns() - begin > limit_ns)) return false;
+        return true;
+    };
+    bool failed = false, lost = false;              // a wait ran out: no more copies, the rows from here on are NaN; lost: one for the team
+    // Barrier of the team.  (Its limit leaves the others time to give up a copy of theirs.)
+    uint32_t team_phase = 0u;
+    auto team_sync = [&]() {
+        __syncwarp();
+        if (lost) return;
+        const uint32_t bar = ptx::smem_u32(&team_bar[team == W ? 0 : 1 + team_no]);
+        if (lane == 0) ptx::mbar_arrive(bar);
+        if (passed(bar, team_phase, 4 * prm.wait_limit_ns + 50000000u)) team_phase ^= 1u;
+        else failed = lost = true;
+    };
 
     // Query fragments of a row, as they lie in memory: the right operand (columns = heads g of the block).  INT8: fragment
     // 4 j + w holds features 16 (t + 4 j) + 4 w .. + 3, as the codes come.
@@ -440,7 +474,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     };
     auto prepare = [&]() {
         while (next_start >= next_end && ic.left > 0) {
-            next_row(ic, prm, unit_shift);
+            next_row(ic, prm, unit_shift, prm.skew_copies);
             if (ic.left > 0) enter_row();
         }
         if (next_start >= next_end) return;
@@ -479,17 +513,6 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
         if (++fill == kStages) fill = 0;
         next_start += unit_keys;
         prepare();
-    };
-    // Bounded wait for the chunk in `stage`; the verdict is the warp's (a copy may land for some lanes as others give up, and
-    // what follows takes the whole warp).
-    auto landed = [&](int stage, uint32_t phase) -> bool {
-        const uint32_t bar = ptx::smem_u32(&full_bar[warp][stage]);
-        if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, phase))) return true;
-        const uint64_t begin = ptx::globaltimer_ns();
-        uint32_t spins = 0;
-        while (!__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, phase)))
-            if ((++spins & 63u) == 0u && __any_sync(0xffffffffu, ptx::globaltimer_ns() - begin > prm.wait_limit_ns)) return false;
-        return true;
     };
     if (ic.left > 0) {
         enter_row();
@@ -546,7 +569,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
     const uint32_t v_at1 = C::kVOff + (D == 128 ? code_piece<D>(v_row1, g) : code_piece<D>(v_row1, g >> 1) + 8 * (g & 1));
     int stage = 0, taken = 0;
     uint32_t phase = 0u;
-    bool failed = false, first_segment = true;      // failed: a wait ran out; no more copies, the rows from here on are NaN
+    bool first_segment = true;
 #pragma unroll 1
     while (cc.left > 0) {
         // ------------------------------------------------ a row, or this worker's part of it
@@ -600,7 +623,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 
 #pragma unroll 1
         for (int start = (cc.unit << unit_shift) + (member << chunk_shift); start < end; start += unit_keys) {
-            if (!failed && !landed(stage, phase)) failed = true;
+            if (!failed && !passed(ptx::smem_u32(&full_bar[warp][stage]), phase, prm.wait_limit_ns)) failed = true;
             if (failed) break;
             any = true;
             const int live = min(chunk, cc.len - start);      // keys of the chunk
@@ -851,7 +874,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
         first_segment = first_segment && none;
         cc.left -= u_end - cc.unit + work.extra;
         if (cc.left > 0) {
-            next_row(cc, prm, unit_shift);
+            next_row(cc, prm, unit_shift, 0);
             if (cc.left > 0) fetch_q(cc);                     // (on the way during the merge)
         }
         if (none) continue;                                   // (a run that begins behind the units of a row)
@@ -895,6 +918,7 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
                 zz[0] += zw[w].x * mw[w].x; zz[1] += zw[w].y * mw[w].y;
                 mw[w].x *= refs[w]; mw[w].y *= refs[w];
             }
+            if (lost) zz[0] = zz[1] = NAN;
             constexpr int kMost = D / 16 / C::kMinTeam;
             float4 o[kMost];
 #pragma unroll
@@ -927,8 +951,8 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
         }
         if (any && !failed) fire();
     }
-    if (failed) {
-        // the copies that are still on the way land before the shared memory is given back
+    if (taken < issued) {
+        // a wait ran out: the copies that are still on the way land before the shared memory is given back
         for (int i = taken; i < issued; ++i) {
             if (i == prm.drop_chunk) continue;
             for (int spin = 0; spin < (1 << 16); ++spin)
@@ -972,7 +996,10 @@ paged_join_kernel(const PagedDecodeParams prm) {
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
     const int4 job = __ldcg(prm.join + blockIdx.x);
-    if (job.x < 0) return;
+    // (a job that no part of the step wrote, see length_of, is what the workspace held)
+    if (static_cast<unsigned>(job.x) >= static_cast<unsigned>(prm.c.B * prm.HG) || static_cast<unsigned>(job.w) > static_cast<unsigned>(prm.workers) ||
+        static_cast<unsigned>(job.z) > static_cast<unsigned>(prm.workers - job.w) || static_cast<unsigned>(job.y) >= 2u * prm.workers)
+        return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, parts = job.w + 1;
     constexpr int F = (D / 16) * NB;
     const int f_begin = blockIdx.y * F / gridDim.y, f_end = (blockIdx.y + 1) * F / gridDim.y;
@@ -1158,7 +1185,7 @@ int tilemix_paged_decode(const tilemix_paged_t* p, int32_t heads_q, float softma
     if ((rc = row_strides(q_stride, p->batch, heads_q, p->head_dim, false, prm.qs))) return rc;
     if ((rc = row_strides(out_stride, p->batch, heads_q, p->head_dim, true, prm.os))) return rc;
     if (workspace_bytes < plan.total) return TILEMIX_ERR_WORKSPACE;
-    prm.wave = plan.wave; prm.jobs = plan.jobs;
+    prm.wave = plan.wave; prm.jobs = plan.jobs; prm.workers = plan.workers;
     prm.Hq = heads_q; prm.R = heads_q / p->heads_kv; prm.groups = plan.groups; prm.HG = plan.HG;
     prm.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(p->head_dim))) * kLog2e;
     prm.q = static_cast<const uint8_t*>(q);
@@ -1170,7 +1197,10 @@ int tilemix_paged_decode(const tilemix_paged_t* p, int32_t heads_q, float softma
     prm.part_o = reinterpret_cast<float4*>(ws + plan.join_bytes + plan.mz_bytes);
     prm.jobs_by_row = static_cast<int64_t>(plan.HG) * p->batch <= plan.workers ? 1 : 0;
     prm.wait_limit_ns = g_wait_limit_ns.load();
-    prm.drop_chunk = g_test_drop.load() == 2 ? 1 : -1;
+    const int drop = g_test_drop.load();
+    prm.drop_chunk = drop == 2 ? 1 : -1;
+    prm.skew = drop == 4 ? 16 : drop == 5 ? 4096 : 0;
+    prm.skew_copies = drop == 6 ? 4096 : drop == 7 ? -4096 : 0;
     const bool int8 = p->cache_type == TILEMIX_CACHE_INT8;
     Launch go;
     if (p->act_type == TILEMIX_TYPE_FP16) go = p->head_dim == 128 ? pick<__half, 128>(int8, plan.NB) : pick<__half, 64>(int8, plan.NB);

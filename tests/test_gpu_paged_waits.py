@@ -42,3 +42,34 @@ def test_short_limits(act, int8, d, hq):
                 assert torch.equal(r["out"][~gone], good["out"][~gone]) and torch.equal(r["lse"][~gone], good["lse"][~gone])
     again = t.tilemix_paged_decode(c, q, want_lse=True)
     assert torch.equal(again["out"], good["out"]) and torch.equal(again["lse"], good["lse"])
+
+
+@pytest.mark.parametrize("act,int8,d,hq,lens", [
+    ("fp16", True, 128, 8, [10, 40000, 12, 3000, 0, 700]), ("bf16", False, 64, 8, [9000] * 30 + [17, 0, 5000]),
+    ("fp16", False, 128, 128, [1 + 37 * i % 700 for i in range(150)]), ("bf16", True, 64, 24, [1 + 41 * i % 300 for i in range(400)]),
+    ("fp16", True, 64, 8, [50 + i for i in range(64)]), ("bf16", False, 128, 8, [16000] * 40)])
+@pytest.mark.parametrize("which", [4, 5, 6, 7])
+def test_lengths_that_warps_do_not_agree_on(act, int8, d, hq, lens, which):
+    """As if the lengths had changed while the call ran: teams of other sizes, other rows, other numbers of barriers and chunks
+    from warp to warp.  The call ends, nothing outside its buffers is touched, and the next call is in order."""
+    t = tm()
+    s = ref.Setup(act, int8, d, 16, 8, lens, seed=3, room=1, device=DEV)
+    q, c = query(s, hq), s.cache()
+    good = t.tilemix_paged_decode(c, q, want_lse=True)
+    ref.check_decode(s, q, good, only=[(b, h) for b in (0, 2, len(lens) - 1) for h in (0, hq - 1)])
+    size = t.tilemix_paged_decode_workspace_size(c, hq)
+    ws = torch.full((size + 4096,), 0x37, dtype=torch.uint8, device=DEV)
+    big = torch.full((q.numel() + 4096,), 5.0, dtype=s.act, device=DEV)
+    out = big[2048:2048 + q.numel()].view(q.shape)
+    pools = [x.clone() for x in (s.k_pool, s.v_pool)]
+    t.tilemix_test_drop_copy(which, 1_000_000)
+    try:
+        for _ in range(2):
+            t.tilemix_paged_decode(c, q, out=out, workspace=ws[:size], want_lse=True)
+        torch.cuda.synchronize()
+    finally:
+        t.tilemix_test_drop_copy(0)
+    assert (ws[size:] == 0x37).all() and (big[:2048] == 5).all() and (big[2048 + q.numel():] == 5).all()
+    assert torch.equal(pools[0], s.k_pool) and torch.equal(pools[1], s.v_pool)
+    again = t.tilemix_paged_decode(c, q, workspace=ws[:size], want_lse=True)
+    assert torch.equal(again["out"], good["out"]) and torch.equal(again["lse"], good["lse"])
