@@ -203,26 +203,21 @@ struct Work {
     Cursor at;
     int team_shift, chunk_shift, worker;
     int base, longer;                        // units of a share; the first `longer` shares have one more
-    int pieces_shift, small;                 // pieces of a share: the first, and others of `small` units
+    int pieces_shift, small;                 // 0: a share is one worker's; 1: two workers', the second one's are its last `small` units
     int extra;                               // units that a row counts as beyond its own, behind them
 
     __device__ __forceinline__ int share_first(int i) const { return i * base + min(i, longer); }
     __device__ __forceinline__ int units_of(int w) const {
-        if ((w & ((1 << pieces_shift) - 1)) != 0) return small;
-        return base + ((w >> pieces_shift) < longer ? 1 : 0) - ((1 << pieces_shift) - 1) * small;
+        if (w & pieces_shift) return small;
+        return base + ((w >> pieces_shift) < longer ? 1 : 0) - small;
     }
     __device__ __forceinline__ int first_of(int w) const {
-        const int i = w >> pieces_shift, j = w & ((1 << pieces_shift) - 1);
-        return j == 0 ? share_first(i) : share_first(i + 1) - ((1 << pieces_shift) - j) * small;
+        const int i = w >> pieces_shift;
+        return w & pieces_shift ? share_first(i + 1) - small : share_first(i);
     }
     __device__ __forceinline__ int worker_of(int unit) const {
         const int split = longer * (base + 1), i = unit < split ? unit / (base + 1) : longer + (unit - split) / base;
-        int w = i << pieces_shift;
-        if (pieces_shift != 0) {
-            const int behind = unit - (share_first(i + 1) - ((1 << pieces_shift) - 1) * small);
-            if (behind >= 0) w += 1 + behind / small;
-        }
-        return w;
+        return (i << pieces_shift) + (pieces_shift != 0 && unit >= share_first(i + 1) - small ? 1 : 0);
     }
 };
 // (fewer than 4, 8, 16: 64 x 500 BF16 31.7 / 32.0 / 33.0 us, 32 x 2K INT8, one query head a KV head, heads of 64
@@ -233,7 +228,7 @@ constexpr int kShortRow = 8;
 // done first: blocks behind the first wave.  (us without and with: 64 ragged FP16 steps, heads of 64 97.4 / 92.8, 16 x 32K BF16
 // 161.2 / 159.7; a block's entry costs as much as that gains where shares are short, 16 x 4K BF16, sixteen query heads
 // 37.1 / 42.9, and in the INT8 form, 8 x 32K 93.2 / 97.0.)
-constexpr int kPiecesShift = 1, kLongShare = 32;
+constexpr int kLongShare = 32;
 // The start of a row and its merge cost a worker as much as some blocks of 16 keys; unless shares are short, a row counts as
 // that many more, or the workers with the most rows end last.  (us with 0, 2, 4, 6 blocks: 64 x 500 BF16 35.4 / 32.0 / 31.9 /
 // 31.9, 200 x 300 BF16, heads of 64 22.7 / 19.5 / 19.2 / 19.4, 256 short INT8, heads of 64 24.5 / 24.5 / 23.3 / 23.3, 32 x 4K
@@ -241,7 +236,8 @@ constexpr int kPiecesShift = 1, kLongShare = 32;
 constexpr int kRowBlocks = 4;
 template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE, bool PIECES>
 __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
-    constexpr int kTeamShift = W == 8 ? 3 : 2, kMinShift = MIN_TEAM == 2 ? 1 : 2;
+    static_assert(W == 4 && MIN_TEAM == 2, "teams of four or two warps");
+    constexpr int kTeamShift = 2, kMinShift = 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = prm.c.B, ctas = prm.wave;
     // (the lengths of the first 256 sequences stay in registers: the loads wait for memory once)
     constexpr int kKept = 8;
@@ -275,10 +271,9 @@ __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
     if (n > 0) { w.base = U / n; w.longer = U - w.base * n; }
     const int block = blockIdx.x;
     if (PIECES && gridDim.x > ctas && w.team_shift == kTeamShift && w.base >= kLongShare) {
-        w.pieces_shift = kPiecesShift;
+        w.pieces_shift = 1;
         w.small = w.base >> 3;
-        // (blocks behind the first wave: one small piece of every share, then the next of every share)
-        w.worker = block < ctas ? block << kPiecesShift : (block % ctas << kPiecesShift) + block / ctas;
+        w.worker = block < ctas ? 2 * block : 2 * (block - ctas) + 1;
     } else {
         w.worker = block < ctas ? (block << (kTeamShift - w.team_shift)) + (warp >> w.team_shift) : 0x40000000;
         if (w.worker >= n) return w;
@@ -1055,7 +1050,7 @@ paged_join_kernel(const PagedDecodeParams prm) {
 // Shape of a launch by instance: what resolve_decode has to know of Cfg.
 struct Plan {
     int NB, groups, HG, wave, ctas, jobs, splits;      // splits: whether a row can have more units than one
-    int team, workers;                           // smallest team; workers that there may be
+    int workers;                                 // workers that there may be
     size_t join_bytes, mz_bytes, total;
 };
 
@@ -1091,9 +1086,9 @@ int resolve_decode(const tilemix_paged_t* p, int heads_q, PagedCache* c, Plan* p
     plan->wave = static_cast<int>(units < wave ? units : wave);
     // blocks behind the first wave, see find_work (which sees the lengths: where shares are short, they return at once)
     const bool pieces = !int8 && rows * (c->capacity / (ch * W)) >= static_cast<int64_t>(kLongShare) * wave;
-    plan->ctas = pieces ? wave << kPiecesShift : plan->wave;
+    plan->ctas = pieces ? 2 * wave : plan->wave;
     plan->splits = c->capacity > 16 * min_team;
-    plan->workers = plan->wave * (W / min_team) > plan->ctas ? plan->wave * (W / min_team) : plan->ctas;
+    plan->workers = plan->wave * (W / min_team);         // (at least as many as CTAs)
     plan->jobs = static_cast<int>(rows < plan->workers ? rows : plan->workers);
     plan->join_bytes = (plan->jobs * sizeof(int4) + 255) / 256 * 256;
     plan->mz_bytes = (static_cast<size_t>(plan->workers) * 2 * 8 * plan->NB * sizeof(float2) + 255) / 256 * 256;
