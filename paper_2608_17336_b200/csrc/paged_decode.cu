@@ -1142,7 +1142,7 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     // warps of one block (64 rows of seven parts: 1.5 us so, 7 in large blocks, which an SM holds one of)
     const bool few = prm.jobs_by_row && static_cast<int64_t>(plan.jobs) * kJoinAtOnce < plan.wave;
     constexpr int kFew = 16, kMany = 4, F = (D / 16) * NB;
-    cfg.gridDim = dim3(plan.jobs, few ? F : plan.jobs * (F / kMany) <= 5 * kSms ? F / kMany : 1); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
+    cfg.gridDim = dim3(plan.jobs, few ? F : F / kMany); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
     e = few ? cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kFew>, prm) : cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D, INT8, NB, kMany>, prm);
     g_launch_count.fetch_add(1);
     return static_cast<int>(e);
