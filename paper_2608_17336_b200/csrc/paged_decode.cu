@@ -92,11 +92,6 @@ struct Cfg {
     static constexpr int kChShift = CH == 16 ? 4 : CH == 32 ? 5 : 6;
     static_assert(CH == 1 << kChShift, "chunks are whole boxes");
     static constexpr int MB = CH / 16;                              // blocks of 16 keys
-    // Blocks that a warp takes together, where a chunk has them whole: what does not depend on their number is done once for two.
-    // (us together and one by one: 64 ragged FP16 steps, heads of 64 97 / 98, 16 x 8K INT8, heads of 64 32.6 / 36.6, 1 x 128K INT8,
-    // sixteen query heads 27.3 / 28.7; 8 x 32K INT8, heads of 128 98 / 93 on a cool GPU, but 104 / 107 at the clock that the power
-    // cap leaves after half a second, where every instruction counts.)
-    static constexpr int kTogether = MB == 1 ? 1 : 2;
     static constexpr int kVOff = CH * D * kElt;                     // values behind the keys of a stage
     static constexpr int kBoxCols = INT8 ? 1 : D / 64;              // boxes side by side in a row of 16-bit values
     static constexpr int kScaleBytes = INT8 ? W * kStages * CH * 8 : 0;
@@ -118,6 +113,13 @@ struct Cfg {
     // 97.9 / 97.6, at the clock that the power cap leaves 102.6 / 95.5, 32 x 4K 39.2 / 36.8, 64 x 500 26.7 / 25.0, 256 short, heads of
     // 64 24.2 / 23.4.)
     static constexpr bool kTwoHalves = !kScaledQ;
+    // Blocks that a warp takes together, where a chunk has them whole: what does not depend on their number is done once for two.
+    // (us together and one by one: 64 ragged FP16 steps, heads of 64 97 / 98, 8 x 32K INT8, heads of 64 51.7 / 55.3, 16 x 8K
+    // 32.8 / 34.9, 256 short ones 24.7 / 25.8, 16 x 4K INT8, sixteen query heads 28.2 / 29.2.)  Heads of 128 over INT8 with
+    // probabilities as two numbers: one by one, which needs no registers beyond those of three CTAs an SM (2 x 32K 35.5 / 33.9,
+    // 1 x 8000 12.5 / 11.8, 32 x 100 12.5 / 11.2, 32 x 4K 40.1 / 39.1, 8 x 32K 97.0 / 91.2, but 105.1 / 106.9 at the clock that the
+    // power cap leaves after half a second).
+    static constexpr int kTogether = MB == 1 || (INT8 && D == 128 && NB == 1 && kTwoHalves) ? 1 : 2;
     static_assert(kFrag * 16 <= kStageBytes, "a row's O of one warp fits the stage that the warp has just read");
 };
 constexpr float kNoMax = -3.4028234663852886e38f;        // running maximum before the first key (finite: nothing is subtracted from an infinity)
