@@ -234,7 +234,9 @@ constexpr int kLongShare = 32;
 // The start of a row and its merge cost a worker as much as some blocks of 16 keys; unless shares are short, a row counts as
 // that many more, or the workers with the most rows end last.  (us with 0, 2, 4, 6 blocks: 64 x 500 BF16 35.4 / 32.0 / 31.9 /
 // 31.9, 200 x 300 BF16, heads of 64 22.7 / 19.5 / 19.2 / 19.4, 256 short INT8, heads of 64 24.5 / 24.5 / 23.3 / 23.3, 32 x 4K
-// INT8 37.2 / 36.8 / 36.8 / 37.7.)
+// INT8 37.2 / 36.8 / 36.8 / 37.7.  Where a worker has no more units than two rows' extra ones, a row would be dealt to fewer
+// workers than there are: counted always and by that rule, 1 x 500 INT8 7.8 / 6.9, 1 x 2000 FP16 10.2 / 10.1; but 1 x 8000 INT8
+// 12.0 / 12.5, 16 x 1K 17.0 / 18.3.)
 constexpr int kRowBlocks = 4;
 template <int W, int CH_SHIFT, int MIN_TEAM, int WAVE, bool PIECES>
 __device__ __forceinline__ Work find_work(const PagedDecodeParams& prm) {
@@ -1141,7 +1143,10 @@ int launch(const PagedDecodeParams& prm, const Plan& plan, cudaStream_t stream) 
     g_launch_count.fetch_add(1);
     if (e != cudaSuccess || !plan.splits) return static_cast<int>(e);
     // few rows: many parts each, a block of sixteen warps for a fragment; otherwise the parts of a row go at once, to the
-    // warps of one block (64 rows of seven parts: 1.5 us so, 7 in large blocks, which an SM holds one of)
+    // warps of two blocks (64 rows of seven parts: 1.5 us so, 7 in large blocks, which an SM holds one of).  (Whole calls, us,
+    // large blocks up to 55 rows (36 with sixteen query heads) / never / up to 110 (73): 1 x 128K INT8, 2 rows 27.1 / 45.1 / 27.2,
+    // 1 x 8000, 8 rows 12.5 / 17.8 / 12.5, 2 x 32K, 16 rows 35.3 / 37.3 / 35.3, 4 x 20K BF16, 32 rows 62.4 / 61.2 / 62.3, 4 x 2K,
+    // 32 rows 14.1 / 12.1 / 14.1, 8 x 32K, 64 rows 97.2 / 97.3 / 101.7, 12 x 2K FP16, 96 rows 24.9 / 24.9 / 31.3.)
     const bool few = prm.jobs_by_row && static_cast<int64_t>(plan.jobs) * kJoinAtOnce < plan.wave;
     constexpr int kFew = 16, kMany = 4, F = (D / 16) * NB;
     cfg.gridDim = dim3(plan.jobs, few ? F : F / kMany); cfg.blockDim = dim3(32 * (few ? kFew : kMany)); cfg.dynamicSmemBytes = 0;
