@@ -390,8 +390,10 @@ int tilemix_paged_append(const tilemix_paged_t* c, int32_t n_tokens, const void*
                          const void* v_new, const int64_t* v_new_stride, const int32_t* cu_new, void* stream);
 
 /* Reads tokens [start[b], cache_len[b]) of every sequence back, as act_type: the FP32 product x8 * delta, rounded
- * (16-bit caches: a copy).  The dense form is what tilemix_attention_fwd_chunk takes as K and V, the packed one what the variable-length calls
- * take.
+ * (16-bit caches: a copy).  As FP16 the dense form is what tilemix_attention_fwd_chunk takes as K and V (one kv_len for all of
+ * its batch: sequences of unequal lengths are a call each), the packed one what the variable-length calls take; those calls take
+ * FP16 alone.  An INT8 cache of a BF16 model can be described a second time, with act_type FP16, to be read back for them; a
+ * 16-bit BF16 cache has decode, but no prefill here.
  *   start     int32 [batch] on the device, or NULL = 0 (values below 0 count as 0)
  *   cu_out    NULL: dense outputs [batch, Hk, out_rows, d], token start[b] + i of sequence b in row i; tokens past
  *             out_rows are left out.  Otherwise int32 [batch + 1] on the DEVICE (as cu_new): packed outputs
@@ -407,6 +409,8 @@ int tilemix_paged_gather(const tilemix_paged_t* c, const int32_t* start, const i
  * with the values that the cache stands for; queries are not quantised.  FP32 scores, statistics and sums; for the product
  * with V a probability is the sum of two 16-bit numbers, over an INT8 cache with BF16 outputs one FP16 number (three bits more
  * than the output has).
+ * Scores of any finite size are right to their FP32 rounding.  Sums in FP32 have to stay finite: sum |q k| of a score (BF16
+ * over INT8: key scales below 2^98), and length * 2^8 * max|v|.
  *   heads_q   any multiple of heads_kv
  *   softmax_scale  <= 0 means 1/sqrt(head_dim)
  *   q, out    [batch, Hq, d] in act_type; strides in elements for (batch, head), NULL = dense; 16-byte multiples

@@ -3,9 +3,9 @@
 // HBM-bound: a cached (token, KV head) is 4 d bytes (16-bit cache) or 2 (d + 4) (INT8 codes and scales), read once, and serves
 // the R = H_q / H_k query heads of its group with 4 R d multiply-adds, far below the tensor cores' rate for R <= 16.  Hence
 // warp-level MMAs: their operands pass through registers, where INT8 codes become FP16 and where a key past the end is masked,
-// at the cost of ~21 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.  16 x 32K keys of 128,
-// four KV heads, BF16: 162 us, 6.3 TB/s; 8 x 32K, eight KV heads, INT8: 97 us, 5.7 TB/s, both under the power cap; one
-// sequence of 500 keys 6.8 us, of which the step's latencies are 4 and the joining kernel's 2.
+// at the cost of ~25 instructions a token (INT8, d = 128) where HBM leaves an SM ~43 issue slots a token.  16 x 32K keys of 128,
+// four KV heads, BF16: 159 us, 6.5 TB/s; 8 x 32K, eight KV heads, INT8: 91 us, 6.1 TB/s, 107 at the clock that the power cap
+// leaves after half a second; one sequence of 500 keys 7.1 us, of which the step's latencies are 4 and the joining kernel's 2.
 //
 // Layout of the work.  A warp owns a ring of stages, starts its own copies and takes CHUNKS of 16 to 64 keys, which one TMA box
 // a page brings in, swizzled; no warp waits for another but at the end of a row.  Four warps are a CTA, three CTAs share an SM
@@ -603,8 +603,8 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
             }
         }
 
-        // sub = kOff less the running maximum, which is rounded up to a whole number: exponents lose nothing by it, and what
-        // has been summed is brought to another maximum exactly.
+        // sub = kOff less the running maximum, which is rounded up to a whole number: what has been summed is brought to another
+        // maximum exactly, and an exponent, below 16, is rounded by 2^-21 at most.  (Above kExact: see there.)
         float sub[NB][2], z[NB][2], acc[D / 16][NB][4];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -963,8 +963,8 @@ paged_decode_kernel(const PagedDecodeParams prm, const __grid_constant__ PoolMap
 
 // Joins the parts of the rows that several workers shared.  A job (row, s, w, n) names slot s and the first slots of n workers
 // from w on.  (A kernel of its own, whose launch overlaps the step: the last CTA of a row joining it at its end, found by a
-// counter or by words that the others set, waits for fences and atomics longer than a grid does for its predecessor: one
-// sequence of 500 keys 6.6 us so, 11.0 and 9.0 that way, 8 x 32 K 98, 104, 104.)  What bounds it is the round trips: the parts
+// counter or by words that the others set, waits for fences and atomics longer than a grid does for its predecessor: measured
+// together, one sequence of 500 keys 6.6 us so, 11.0 and 9.0 that way, 8 x 32 K 98, 104, 104.)  What bounds it is the round trips: the parts
 // are loaded kJoinAtOnce at a time.  A row of up to twice as many has a warp for every fragment; the parts of others are shared
 // out over the warps, fragment by fragment (by a block each where rows are few).
 constexpr int kJoinAtOnce = 8;
